@@ -352,6 +352,146 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
                     const float *dq, const float *dk, const float *dv, const float *dg,
                     const pgf_la_params *p, float *o, float *do_, void *stream);
 
+/* ------------------------------------------------------------------------
+ * The gated delta rule: a linear recurrence whose transition is not
+ * diagonal.  Per sequence and value head the state is a d_key x d_value
+ * matrix S; a step with query q, key k, value v, log-decay g and write
+ * strength beta does
+ *   S <- e^g S,   u = beta (v - S^T k),   S <- S + k u^T,   o = scale S^T q,
+ * that is S_t = e^{g_t} (I - beta_t k_t k_t^T) S_{t-1} + beta_t k_t v_t^T.
+ * Keys are meant to be normalised (pgf_qk_norm); with beta |k|^2 <= 2 and
+ * g <= 0 the state stays bounded.  g = -inf forgets the whole state.
+ *
+ * Arrays have the logical shapes
+ *   q, k [B, key_heads, L, d_key]     v, o [B, value_heads, L, d_value]
+ *   g, beta [B, value_heads, L] (f32)
+ *   S [sequences, value_heads, d_key, d_value] (f32, dense row-major)
+ * with value_heads a multiple of key_heads: value head h reads the q and k of
+ * key head h / (value_heads / key_heads).  Each of q, k, v, g, beta, o and the
+ * gradients has strides in elements for batch, head and step ({0, 0, 0}: dense
+ * row-major); the last index is dense.  A stride of zero broadcasts an input.
+ * q, k, v, o and their gradients are f32 or bf16 (in_dtype); the arrays'
+ * addresses and strides are multiples of 16 bytes (g and beta: of 4).
+ *
+ * Packed sequences: with n_seqs > 0, batch is 1 and the rows of the one
+ * batch entry hold n_seqs sequences; sequence n has the rows cu_seqlens[n]
+ * <= t < cu_seqlens[n + 1] (device, int32, n_seqs + 1 ascending values in
+ * 0 .. L; values outside are clipped).  Rows of no sequence are neither read
+ * nor written.  Without it every batch entry is a sequence of L steps.
+ *
+ * The scan works in chunks of 32 steps: products of the chunk's keys among
+ * themselves and with the state on the matrix cores.  bf16 operands enter as
+ * they are, every f32 operand (state, decays, inner results) as a sum of
+ * three bf16 numbers (two where the result is rounded to bf16), so sums and
+ * states have f32 accuracy.  A value that is not finite may reach the outputs
+ * of its own chunk of 32 steps, but no earlier chunk, other sequence or head.
+ * Results do not change from run to run. */
+typedef struct pgf_gdr_params {
+    /* Sizes.  batch, key_heads >= 1; value_heads a multiple of key_heads;
+     * seqlen >= 0; d_key a multiple of 8, at most 128; d_value a multiple of
+     * 8, at most 4096. */
+    int64_t batch, key_heads, value_heads, seqlen, d_key, d_value;
+    int64_t n_seqs;                 /* packed sequences, 0 = one per batch entry */
+    const int32_t *cu_seqlens;      /* device, [n_seqs + 1]; NULL when n_seqs is 0 */
+    int32_t in_dtype;               /* PGF_F32 or PGF_BF16                        */
+    /* Steps per segment: sequences are cut into segments whose transitions
+     * are composed, so that they run side by side.  0 = library default, -1 =
+     * not cut, else a multiple of 32. */
+    int32_t seg_len;
+    float scale;
+    int32_t grads;                  /* planning calls: 1 = of pgf_gdr_grads       */
+    int64_t q_strides[3], k_strides[3], v_strides[3], g_strides[3], beta_strides[3];
+    int64_t o_strides[3];           /* o; pgf_gdr_grads: the adjoint signal do_   */
+    int64_t dq_strides[3], dk_strides[3], dv_strides[3];
+    /* Entry states (NULL = zero) and final states (NULL = not written). */
+    const float *S_in;
+    float *S_out;
+    /* pgf_gdr_grads: dl/dS_out (NULL = zero) and dl/dS_in (NULL = not written). */
+    const float *dS_out;
+    float *dS_in;
+    /* pgf_gdr_step: the pool of states, its number of states, and the state of
+     * each batch entry (device, int32 [batch]; NULL = entry b has state b). */
+    float *S_pool;
+    int64_t pool;
+    const int32_t *slots;
+    /* Scratch (device), at least pgf_gdr_workspace_bytes(p), 256-byte aligned.
+     * It grows with the number of steps.  Not used by pgf_gdr_step. */
+    void *workspace;
+    size_t workspace_bytes;
+} pgf_gdr_params;
+
+/* Workspace bytes of pgf_gdr_scan, or of pgf_gdr_grads with p->grads = 1
+ * (0 if invalid or unsupported).  Host only. */
+size_t pgf_gdr_workspace_bytes(const pgf_gdr_params *p);
+
+/* Steps per segment that a call with these sizes takes (0: sequences are not
+ * cut) in *seg_len.  Host only.  Returns a status. */
+int pgf_gdr_plan(const pgf_gdr_params *p, int32_t *seg_len);
+
+/* The scan over whole sequences.  o must not overlap an input, nor the
+ * workspace anything. */
+int pgf_gdr_scan(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                 const pgf_gdr_params *p, void *o, void *stream);
+
+/* A few steps in place on a pool of states: entry b advances S_pool[slots[b]]
+ * by its L steps (any L, made for one to a few) and writes its o.  An entry
+ * whose slot is not in 0 .. pool - 1, or is that of an earlier entry, is
+ * padding: its outputs are zero and no state changes.  n_seqs must be 0. */
+int pgf_gdr_step(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                 const pgf_gdr_params *p, void *o, void *stream);
+
+/* ------------------------------------------------------------------------
+ * Preparation of queries and keys: per head and step
+ *   y = R(position) (w * x r),   r = 1 / sqrt(c sum_i x_i^2 + eps),
+ * c = 1 (PGF_NORM_L2) or 1 / d (PGF_NORM_RMS), or r = 1 (PGF_NORM_NONE); w is
+ * a weight per element (f32, NULL = 1).  R turns the pair (a, b) number i of
+ * the first `rot` elements by the angle position * inv_freq[i]: the pairs are
+ * the elements i and i + rot / 2, or 2 i and 2 i + 1 with `interleaved`.
+ * Sums and angles are f32 (the angle's reduction f64), so far positions keep
+ * their accuracy.
+ *   q, q_out [B, q_heads, L, d]    k, k_out [B, k_heads, L, d]
+ * with strides as in the gated delta rule.  Either of q and k may be left out
+ * (its heads 0).  An output may be its input (same address and strides).
+ * ------------------------------------------------------------------------ */
+#define PGF_NORM_NONE 0
+#define PGF_NORM_L2   1
+#define PGF_NORM_RMS  2
+
+typedef struct pgf_qk_params {
+    /* d_head a multiple of 8, at most 512; rot a multiple of 16, at most
+     * d_head (0: no rotation). */
+    int64_t batch, q_heads, k_heads, seqlen, d_head, rot;
+    int32_t in_dtype;               /* PGF_F32 or PGF_BF16                       */
+    int32_t norm;                   /* PGF_NORM_*                                */
+    int32_t interleaved;
+    float eps;
+    int64_t q_strides[3], k_strides[3], q_out_strides[3], k_out_strides[3];
+    int64_t dq_strides[3], dk_strides[3];           /* pgf_qk_norm_grads: the adjoint signals */
+    const float *w_q, *w_k;         /* device, [d] f32, or NULL                  */
+    const float *inv_freq;          /* device, [rot / 2] f32                     */
+    /* Positions (device), int32 or int64 (pos_bits 32 or 64): that of step t
+     * of batch entry b is positions[b * pos_stride + t]; NULL = t. */
+    const void *positions;
+    int32_t pos_bits;
+    int64_t pos_stride;
+    /* pgf_qk_norm_grads: dl/dw_q and dl/dw_k, device [d] f32, overwritten;
+     * required where the weight is given. */
+    float *grad_w_q, *grad_w_k;
+    /* Scratch of pgf_qk_norm_grads where a weight is given. */
+    void *workspace;
+    size_t workspace_bytes;
+} pgf_qk_params;
+
+/* Workspace bytes of pgf_qk_norm_grads.  Host only. */
+size_t pgf_qk_norm_workspace_bytes(const pgf_qk_params *p);
+
+int pgf_qk_norm(const void *q, const void *k, const pgf_qk_params *p, void *q_out, void *k_out, void *stream);
+
+/* The adjoint: from x (q, k) and dl/dy (dq, dk) to dl/dx in q_out and k_out
+ * and dl/dw.  The sums over steps and heads are added in a fixed order. */
+int pgf_qk_norm_grads(const void *q, const void *k, const void *dq, const void *dk, const pgf_qk_params *p,
+                      void *q_out, void *k_out, void *stream);
+
 /* Static string for a status code. */
 const char *pgf_status_string(int status);
 

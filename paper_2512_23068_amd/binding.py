@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libpgf.so")
 PGF_OK = 0
 PGF_F32 = 0
 PGF_BF16 = 1
+NORMS = {"none": 0, "l2": 1, "rms": 2}
 DRIVES = {"euler": 0, "zoh": 1}
 ACTIVATIONS = {"identity": 0, "silu": 1}
 TIMING_KINDS = ("proj", "seg_aggregate", "carry", "scan_out", "state_io")
@@ -54,6 +55,38 @@ class PgfLaParams(ctypes.Structure):
     ]
 
 
+_i64x3 = ctypes.c_int64 * 3
+
+
+class PgfGdrParams(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int64), ("key_heads", ctypes.c_int64), ("value_heads", ctypes.c_int64),
+        ("seqlen", ctypes.c_int64), ("d_key", ctypes.c_int64), ("d_value", ctypes.c_int64),
+        ("n_seqs", ctypes.c_int64), ("cu_seqlens", _c_f), ("in_dtype", ctypes.c_int32), ("seg_len", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("grads", ctypes.c_int32),
+        ("q_strides", _i64x3), ("k_strides", _i64x3), ("v_strides", _i64x3), ("g_strides", _i64x3),
+        ("beta_strides", _i64x3), ("o_strides", _i64x3), ("dq_strides", _i64x3), ("dk_strides", _i64x3),
+        ("dv_strides", _i64x3),
+        ("S_in", _c_f), ("S_out", _c_f), ("dS_out", _c_f), ("dS_in", _c_f),
+        ("S_pool", _c_f), ("pool", ctypes.c_int64), ("slots", _c_f),
+        ("workspace", _c_f), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class PgfQkParams(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int64), ("q_heads", ctypes.c_int64), ("k_heads", ctypes.c_int64),
+        ("seqlen", ctypes.c_int64), ("d_head", ctypes.c_int64), ("rot", ctypes.c_int64),
+        ("in_dtype", ctypes.c_int32), ("norm", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("q_strides", _i64x3), ("k_strides", _i64x3), ("q_out_strides", _i64x3), ("k_out_strides", _i64x3),
+        ("dq_strides", _i64x3), ("dk_strides", _i64x3),
+        ("w_q", _c_f), ("w_k", _c_f), ("inv_freq", _c_f), ("positions", _c_f), ("pos_bits", ctypes.c_int32),
+        ("pos_stride", ctypes.c_int64), ("grad_w_q", _c_f), ("grad_w_k", _c_f),
+        ("workspace", _c_f), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
 class PgfPlanInfo(ctypes.Structure):
     _fields_ = [
         ("n_per_thread", ctypes.c_int32), ("n_split", ctypes.c_int32), ("seg_len", ctypes.c_int32),
@@ -64,7 +97,9 @@ class PgfPlanInfo(ctypes.Structure):
 
 EXPORTED = ("pgf_workspace_bytes", "pgf_plan", "pgf_scan_jvp", "pgf_scan_jvp_noalloc", "pgf_scan_jvp2",
             "pgf_param_grads",
-            "pgf_la_workspace_bytes", "pgf_la_plan", "pgf_la_scan_jvp", "pgf_status_string", "pgf_timing_enable",
+            "pgf_la_workspace_bytes", "pgf_la_plan", "pgf_la_scan_jvp",
+            "pgf_gdr_workspace_bytes", "pgf_gdr_plan", "pgf_gdr_scan", "pgf_gdr_step",
+            "pgf_qk_norm_workspace_bytes", "pgf_qk_norm", "pgf_qk_norm_grads", "pgf_status_string", "pgf_timing_enable",
             "pgf_timing_read")
 
 _lib = None
@@ -102,6 +137,21 @@ def lib():
     L.pgf_la_plan.argtypes = [LP, ctypes.POINTER(PgfPlanInfo)]
     L.pgf_la_scan_jvp.restype = ctypes.c_int
     L.pgf_la_scan_jvp.argtypes = [ctypes.c_void_p] * 8 + [LP, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
+    GP, QP, V = ctypes.POINTER(PgfGdrParams), ctypes.POINTER(PgfQkParams), ctypes.c_void_p
+    L.pgf_gdr_workspace_bytes.restype = ctypes.c_size_t
+    L.pgf_gdr_workspace_bytes.argtypes = [GP]
+    L.pgf_gdr_plan.restype = ctypes.c_int
+    L.pgf_gdr_plan.argtypes = [GP, ctypes.POINTER(ctypes.c_int32)]
+    L.pgf_gdr_scan.restype = ctypes.c_int
+    L.pgf_gdr_scan.argtypes = [V] * 5 + [GP, V, V]
+    L.pgf_gdr_step.restype = ctypes.c_int
+    L.pgf_gdr_step.argtypes = [V] * 5 + [GP, V, V]
+    L.pgf_qk_norm_workspace_bytes.restype = ctypes.c_size_t
+    L.pgf_qk_norm_workspace_bytes.argtypes = [QP]
+    L.pgf_qk_norm.restype = ctypes.c_int
+    L.pgf_qk_norm.argtypes = [V] * 2 + [QP] + [V] * 3
+    L.pgf_qk_norm_grads.restype = ctypes.c_int
+    L.pgf_qk_norm_grads.argtypes = [V] * 4 + [QP] + [V] * 3
     L.pgf_status_string.restype = ctypes.c_char_p
     L.pgf_status_string.argtypes = [ctypes.c_int]
     L.pgf_timing_enable.restype = ctypes.c_int
@@ -556,6 +606,294 @@ def _la_scan_jvp_on(ts, S_in, dS_in, return_state, seg_len, chunk_segs, workspac
     rc = L_.pgf_la_scan_jvp(*[_ptr(t) for t in ts], ctypes.byref(pr), _ptr(o), _ptr(do), ctypes.c_void_p(st))
     _check(rc)
     return (o, do) + states
+
+
+def _rows(t, shape, dev, name, dtypes):
+    """An input [B, H, L, ..] as the kernels read it: on dev, of one of dtypes,
+    its last index dense and its address and strides in units of 16 bytes (of
+    the element for [B, H, L]); anything else is copied."""
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.dtype in dtypes):
+        raise ValueError(f"{name}: expected a {' or '.join(str(d) for d in dtypes)} tensor on {dev}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    moves = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
+    return t if _in_place(t) and (any(moves) or not moves) else t.clone(memory_format=torch.contiguous_format)
+
+
+def _in_place(t):
+    """Whether the kernels can take t's rows where they are."""
+    if t.numel() == 0 or t.dim() == 3:
+        return True
+    unit = 16 // t.element_size()
+    st = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
+    return (t.stride(3) == 1 or t.shape[3] == 1) and t.data_ptr() % 16 == 0 and all(s % unit == 0 for s in st)
+
+
+def _set_strides(field, t):
+    """Strides of [B, H, L, ..] (of indexes that move)."""
+    field[0], field[1], field[2] = (0 if n <= 1 else s for s, n in zip(t.stride()[:3], t.shape[:3]))
+
+
+def _like_rows(t, shape, dtype):
+    """A new output [B, H, L, d] in the order of t: step-major where t's heads
+    lie side by side in each step."""
+    B, H, L, d = shape
+    if t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) < t.stride(2):
+        return torch.empty((B, L, H, d), device=t.device, dtype=dtype).transpose(1, 2)
+    return torch.empty(shape, device=t.device, dtype=dtype)
+
+
+def _check_rows_out(t, shape, dtype, dev, name):
+    """A caller's output [B, H, L, d] with any strides the kernels can write."""
+    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and tuple(t.shape) == tuple(shape)
+            and _in_place(t) and all(s > 0 for s, n in zip(t.stride(), t.shape) if n > 1)):
+        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on {dev} with dense rows of "
+                         "16-byte aligned address and strides")
+    return t
+
+
+def _state(t, shape, dev, name):
+    """A state the kernels read or write in place (float32, dense)."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.device == dev
+            and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.data_ptr() % 16 == 0):
+        raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {tuple(shape)} on {dev}")
+    return t
+
+
+def _gdr_inputs(q, k, v, g, beta, scale, seg_len):
+    """Checks shapes and fills the common fields; returns (params, tensors)."""
+    if q.dim() != 4 or v.dim() != 4 or k.shape != q.shape:
+        raise ValueError("shapes: q, k [B,Hk,L,dk], v [B,Hv,L,dv], g, beta [B,Hv,L]")
+    if q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q, k and v must all be float32 or all bfloat16")
+    dev, dt = q.device, (q.dtype,)
+    B, Hk, L, dk = q.shape
+    Hv, dv = v.shape[1], v.shape[3]
+    q, k = _rows(q, (B, Hk, L, dk), dev, "q", dt), _rows(k, (B, Hk, L, dk), dev, "k", dt)
+    v = _rows(v, (B, Hv, L, dv), dev, "v", dt)
+    g = _rows(g, (B, Hv, L), dev, "g", (torch.float32,))
+    beta = _rows(beta, (B, Hv, L), dev, "beta", (torch.float32,))
+    p = PgfGdrParams()
+    p.batch, p.key_heads, p.value_heads, p.seqlen, p.d_key, p.d_value = B, Hk, Hv, L, dk, dv
+    p.in_dtype = PGF_BF16 if q.dtype == torch.bfloat16 else PGF_F32
+    p.seg_len = int(seg_len)
+    p.scale = float(dk ** -0.5 if scale is None else scale)
+    for field, t in ((p.q_strides, q), (p.k_strides, k), (p.v_strides, v), (p.g_strides, g),
+                     (p.beta_strides, beta)):
+        _set_strides(field, t)
+    return p, (q, k, v, g, beta)
+
+
+def _gdr_packed(p, cu_seqlens, B, dev):
+    """Sets the packed sequences; returns the number of sequences."""
+    if cu_seqlens is None:
+        return B
+    c = cu_seqlens
+    if not (isinstance(c, torch.Tensor) and c.device == dev and c.dtype == torch.int32 and c.dim() == 1
+            and c.numel() >= 2 and c.is_contiguous()):
+        raise ValueError(f"cu_seqlens: expected a contiguous int32 tensor [sequences + 1] on {dev}")
+    if B != 1:
+        raise ValueError("cu_seqlens: packed sequences take a batch of 1")
+    p.n_seqs, p.cu_seqlens = c.numel() - 1, c.data_ptr()
+    return c.numel() - 1
+
+
+def _gdr_workspace(L_, p, workspace, dev):
+    nbytes = int(L_.pgf_gdr_workspace_bytes(ctypes.byref(p)))
+    if nbytes == 0:
+        _check(L_.pgf_gdr_plan(ctypes.byref(p), ctypes.byref(ctypes.c_int32())))
+    workspace = _checked_workspace(workspace, nbytes, dev)
+    p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    return workspace
+
+
+def _all_on_device(*ts):
+    if not all(isinstance(t, torch.Tensor) and t.is_cuda for t in ts):
+        raise ValueError("q, k, v, g and beta must be device tensors")
+
+
+def gdr_scan(q, k, v, g, beta, *, scale=None, S_in=None, return_state=False, cu_seqlens=None, qk_prep=None, seg_len=0,
+             workspace=None, out=None, stream=None):
+    """The gated delta rule over whole sequences on the GPU.
+
+    q, k [B,Hk,L,dk] and v [B,Hv,L,dv]: all float32 or all bfloat16; Hv a
+    multiple of Hk (value head h reads key head h // (Hv // Hk)); g (log-decay)
+    and beta (write strength) [B,Hv,L] float32.  Any strides: a view of a fused
+    projection is read in place.  scale: of the output, 1/sqrt(dk) by default.
+    cu_seqlens: int32 [sequences + 1] on the device: the rows of the one batch
+    entry hold that many sequences (a new output is zero in the rows of none;
+    a caller's keeps what it held there).
+    S_in: entry states [sequences,Hv,dk,dv] float32.  qk_prep: keyword
+    arguments of qk_norm, which then prepares q and k first.
+    Returns o [B,Hv,L,dv] in q's type, with return_state (o, S_out).
+    """
+    _all_on_device(q, k, v, g, beta)
+    with torch.cuda.device(q.device), _on_stream(stream, q.device):
+        L_ = lib()
+        if qk_prep is not None:
+            q, k = qk_norm(q, k, **qk_prep)
+        p, (q, k, v, g, beta) = _gdr_inputs(q, k, v, g, beta, scale, seg_len)
+        dev = q.device
+        B, Hv, L, dv = v.shape
+        n = _gdr_packed(p, cu_seqlens, B, dev)
+        cell = (n, Hv, q.shape[3], dv)
+        S_in = _state(S_in, cell, dev, "S_in")
+        p.S_in = None if S_in is None else S_in.data_ptr()
+        if out is None:
+            o = _like_rows(v, v.shape, q.dtype)
+            if cu_seqlens is not None:
+                o.zero_()
+        else:
+            o = _check_rows_out(out, v.shape, q.dtype, dev, "out")
+        _set_strides(p.o_strides, o)
+        workspace = _gdr_workspace(L_, p, workspace, dev)
+        S_out = None
+        if return_state:
+            S_out = torch.empty(cell, device=dev, dtype=torch.float32)
+            p.S_out = S_out.data_ptr()
+        st = torch.cuda.current_stream(dev).cuda_stream
+        _check(L_.pgf_gdr_scan(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), ctypes.byref(p), _ptr(o),
+                               ctypes.c_void_p(st)))
+        return (o, S_out) if return_state else o
+
+
+def gdr_step(q, k, v, g, beta, S, *, slots=None, scale=None, qk_prep=None, out=None, stream=None):
+    """A few steps of the gated delta rule in place on a pool of states.
+
+    Inputs as in gdr_scan, with L the steps to advance (one token, or a few
+    drafted ones).  S [pool,Hv,dk,dv] float32, contiguous, is updated in place:
+    entry b advances S[slots[b]] (slots: int32 [B] on the device; None: S[b]).
+    An entry whose slot is not a state of the pool (-1: padding), or is that of
+    an earlier entry, has zero outputs and changes nothing.  Returns o.
+    """
+    _all_on_device(q, k, v, g, beta)
+    with torch.cuda.device(q.device), _on_stream(stream, q.device):
+        L_ = lib()
+        if qk_prep is not None:
+            q, k = qk_norm(q, k, **qk_prep)
+        p, (q, k, v, g, beta) = _gdr_inputs(q, k, v, g, beta, scale, 0)
+        dev = q.device
+        B, Hv, L, dv = v.shape
+        if not isinstance(S, torch.Tensor) or S.dim() != 4:
+            raise ValueError("S: expected states [pool,Hv,dk,dv]")
+        _state(S, (S.shape[0], Hv, q.shape[3], dv), dev, "S")
+        p.S_pool, p.pool = S.data_ptr(), S.shape[0]
+        if slots is not None:
+            if not (isinstance(slots, torch.Tensor) and slots.device == dev and slots.dtype == torch.int32
+                    and tuple(slots.shape) == (B,) and slots.is_contiguous()):
+                raise ValueError(f"slots: expected a contiguous int32 tensor [{B}] on {dev}")
+            p.slots = slots.data_ptr()
+        elif S.shape[0] < B:
+            raise ValueError(f"S: {S.shape[0]} states for {B} entries")
+        o = _like_rows(v, v.shape, q.dtype) if out is None else _check_rows_out(out, v.shape, q.dtype, dev, "out")
+        _set_strides(p.o_strides, o)
+        st = torch.cuda.current_stream(dev).cuda_stream
+        _check(L_.pgf_gdr_step(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), ctypes.byref(p), _ptr(o),
+                               ctypes.c_void_p(st)))
+        return o
+
+
+def _qk_params(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved, keep):
+    """Checks the arguments shared by qk_norm and its adjoint."""
+    if q.dim() != 4 or k.dim() != 4 or (k.shape[0], k.shape[2], k.shape[3]) != (q.shape[0], q.shape[2], q.shape[3]):
+        raise ValueError("shapes: q [B,Hq,L,d], k [B,Hk,L,d]")
+    if q.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("q and k must both be float32 or both bfloat16")
+    if norm not in NORMS:
+        raise ValueError(f"norm: one of {', '.join(NORMS)}")
+    dev = q.device
+    B, Hq, L, d = q.shape
+    q, k = _rows(q, q.shape, dev, "q", (q.dtype,)), _rows(k, k.shape, dev, "k", (q.dtype,))
+    p = PgfQkParams()
+    p.batch, p.q_heads, p.k_heads, p.seqlen, p.d_head = B, Hq, k.shape[1], L, d
+    p.in_dtype = PGF_BF16 if q.dtype == torch.bfloat16 else PGF_F32
+    p.norm, p.eps, p.interleaved = NORMS[norm], float(eps), int(bool(interleaved))
+    wq, wk = _dev_param(wq, (d,), dev, "wq"), _dev_param(wk, (d,), dev, "wk")
+    p.w_q, p.w_k = (None if w is None else w.data_ptr() for w in (wq, wk))
+    if inv_freq is not None:
+        if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+            raise ValueError("inv_freq: expected a tensor [rot / 2]")
+        inv_freq = _dev_param(inv_freq, inv_freq.shape, dev, "inv_freq")
+        p.rot, p.inv_freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
+        if positions is not None:
+            if not (isinstance(positions, torch.Tensor) and positions.device == dev
+                    and positions.dtype in (torch.int32, torch.int64)
+                    and tuple(positions.shape) in ((L,), (1, L), (B, L))):
+                raise ValueError(f"positions: expected int32 or int64 [{L}] or [{B},{L}] on {dev}")
+            if L > 1 and positions.stride(-1) != 1:
+                positions = positions.contiguous()
+            p.positions, p.pos_bits = positions.data_ptr(), 8 * positions.element_size()
+            p.pos_stride = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
+    _set_strides(p.q_strides, q)
+    _set_strides(p.k_strides, k)
+    keep += [wq, wk, inv_freq, positions]
+    return p, q, k
+
+
+def _qk_outputs(p, q, k, out, names):
+    if out is None:
+        qo, ko = _like_rows(q, q.shape, q.dtype), _like_rows(k, k.shape, k.dtype)
+    else:
+        qo, ko = out
+        _check_rows_out(qo, q.shape, q.dtype, q.device, names[0])
+        _check_rows_out(ko, k.shape, k.dtype, q.device, names[1])
+    _set_strides(p.q_out_strides, qo)
+    _set_strides(p.k_out_strides, ko)
+    return qo, ko
+
+
+def qk_norm(q, k, *, wq=None, wk=None, norm="rms", eps=1e-6, positions=None, inv_freq=None, interleaved=False,
+            out=None, stream=None):
+    """Norm of every head's queries and keys, weight and rotation by position.
+
+    q [B,Hq,L,d], k [B,Hk,L,d]: both float32 or both bfloat16, any strides.
+    norm: "rms", "l2" or "none"; wq, wk: weights [d].  inv_freq [rot / 2]: the
+    first rot elements turn in pairs by position * inv_freq (None: no
+    rotation); positions int32 or int64 [L] or [B,L] (None: 0 .. L-1); pairs
+    are (i, i + rot / 2), or (2 i, 2 i + 1) when interleaved.
+    out: optional (q, k) outputs, which may be the inputs themselves.
+    Returns (q, k) prepared, in the inputs' type and order.
+    """
+    if not (isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor) and q.is_cuda and k.is_cuda):
+        raise ValueError("q and k must be device tensors")
+    with torch.cuda.device(q.device), _on_stream(stream, q.device):
+        L_, keep = lib(), []
+        p, q, k = _qk_params(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved, keep)
+        qo, ko = _qk_outputs(p, q, k, out, ("out[0]", "out[1]"))
+        st = torch.cuda.current_stream(q.device).cuda_stream
+        _check(L_.pgf_qk_norm(_ptr(q), _ptr(k), ctypes.byref(p), _ptr(qo), _ptr(ko), ctypes.c_void_p(st)))
+        return qo, ko
+
+
+def qk_norm_grads(q, k, dq, dk, *, wq=None, wk=None, norm="rms", eps=1e-6, positions=None, inv_freq=None,
+                  interleaved=False, workspace=None, out=None, stream=None):
+    """The adjoint of qk_norm: dq and dk are dl/d(its outputs), q and k its inputs.
+
+    Returns dl/dq and dl/dk in the inputs' type, then dl/dwq and dl/dwk [d]
+    float32 for the weights that are given.
+    """
+    if not all(isinstance(t, torch.Tensor) and t.is_cuda for t in (q, k, dq, dk)):
+        raise ValueError("q, k, dq and dk must be device tensors")
+    with torch.cuda.device(q.device), _on_stream(stream, q.device):
+        L_, keep = lib(), []
+        p, q, k = _qk_params(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved, keep)
+        dq, dk = _rows(dq, q.shape, q.device, "dq", (q.dtype,)), _rows(dk, k.shape, q.device, "dk", (q.dtype,))
+        _set_strides(p.dq_strides, dq)
+        _set_strides(p.dk_strides, dk)
+        qo, ko = _qk_outputs(p, q, k, out, ("out[0]", "out[1]"))
+        gw = []
+        for w, field in ((wq, "grad_w_q"), (wk, "grad_w_k")):
+            if w is not None:
+                gw.append(torch.empty(q.shape[3], device=q.device, dtype=torch.float32))
+                setattr(p, field, gw[-1].data_ptr())
+        workspace = _checked_workspace(workspace, int(L_.pgf_qk_norm_workspace_bytes(ctypes.byref(p))), q.device)
+        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
+        st = torch.cuda.current_stream(q.device).cuda_stream
+        _check(L_.pgf_qk_norm_grads(_ptr(q), _ptr(k), _ptr(dq), _ptr(dk), ctypes.byref(p), _ptr(qo), _ptr(ko),
+                                    ctypes.c_void_p(st)))
+        return (qo, ko, *gw)
 
 
 def timing_enable(on: bool = True):

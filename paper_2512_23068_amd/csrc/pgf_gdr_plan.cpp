@@ -1,0 +1,168 @@
+// Host-side planning of the gated delta rule and of the query/key
+// preparation (see pgf_gdr_plan.h).
+#include "pgf_gdr_plan.h"
+
+#include <algorithm>
+
+namespace pgf {
+
+namespace {
+
+constexpr int64_t kMaxBlocks = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxHeads = int64_t(1) << 16, kMaxBatch = int64_t(1) << 24, kMaxLen = int64_t(1) << 32;
+constexpr int64_t kMaxStride = int64_t(1) << 44;
+constexpr size_t kMaxTotal = size_t(1) << 46;
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Strides of an array of rows of `width` elements: not negative, bounded, in
+// units of 16 bytes; an output's rows must not fall on each other.
+bool strides_ok(const int64_t (&s)[3], int64_t unit, bool out, int64_t B, int64_t H, int64_t L) {
+    const int64_t n[3] = {B, H, L};
+    const bool dense = !s[0] && !s[1] && !s[2];
+    for (int i = 0; i < 3; ++i) {
+        if (s[i] < 0 || s[i] > kMaxStride || s[i] % unit) return false;
+        if (out && !dense && n[i] > 1 && !s[i]) return false;
+    }
+    return true;
+}
+
+// Adds a section of n * each bytes; false when the workspace would leave any
+// sensible size.
+bool section(size_t *total, size_t *at, int64_t n, int64_t each) {
+    *at = *total;
+    const double want = (double)n * (double)each;
+    if (want > (double)kMaxTotal) return false;
+    *total += ((size_t)n * (size_t)each + 255) / 256 * 256;
+    return *total <= kMaxTotal;
+}
+
+}  // namespace
+
+void dense_strides(const int64_t (&in)[3], int64_t heads, int64_t L, int64_t width, int64_t (&out)[3]) {
+    const bool dense = !in[0] && !in[1] && !in[2];
+    out[0] = dense ? heads * L * width : in[0];
+    out[1] = dense ? L * width : in[1];
+    out[2] = dense ? width : in[2];
+}
+
+size_t extent(const int64_t (&s)[3], int64_t B, int64_t heads, int64_t L, int64_t width, size_t elem) {
+    if (B < 1 || heads < 1 || L < 1 || width < 1) return 0;
+    int64_t d[3];
+    dense_strides(s, heads, L, width, d);
+    return (size_t)((B - 1) * d[0] + (heads - 1) * d[1] + (L - 1) * d[2] + width) * elem;
+}
+
+bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
+    const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+    return a && b && na && nb && pa < pb + nb && pb < pa + na;
+}
+
+namespace gdr {
+
+int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
+    if (!p || !out) return PGF_ERR_INVALID_ARG;
+    Plan q{};
+    q.B = p->batch; q.Hk = p->key_heads; q.Hv = p->value_heads; q.L = p->seqlen; q.dk = p->d_key; q.dv = p->d_value;
+    if (q.B < 1 || q.Hk < 1 || q.Hv < 1 || q.L < 0 || q.dk < 1 || q.dv < 1 || p->n_seqs < 0) return PGF_ERR_INVALID_ARG;
+    if (p->in_dtype != PGF_F32 && p->in_dtype != PGF_BF16) return PGF_ERR_INVALID_ARG;
+    if (q.Hv % q.Hk) return PGF_ERR_INVALID_ARG;
+    if (q.dk % 8 || q.dk > 128 || q.dv % 8 || q.dv > 4096) return PGF_ERR_UNSUPPORTED;
+    if (q.B > kMaxBatch || q.Hv > kMaxHeads || q.L > kMaxLen || p->n_seqs > kMaxBatch) return PGF_ERR_UNSUPPORTED;
+    if (p->n_seqs && (q.B != 1 || step)) return PGF_ERR_INVALID_ARG;
+    if (p->seg_len < -1 || (p->seg_len > 0 && p->seg_len % kC)) return PGF_ERR_INVALID_ARG;
+    const int64_t unit = p->in_dtype == PGF_BF16 ? 8 : 4;
+    const struct { const int64_t (&s)[3]; int64_t unit; bool out; int64_t heads; } arrays[] = {
+        {p->q_strides, unit, false, q.Hk}, {p->k_strides, unit, false, q.Hk}, {p->v_strides, unit, false, q.Hv},
+        {p->g_strides, 1, false, q.Hv}, {p->beta_strides, 1, false, q.Hv}, {p->o_strides, unit, !grads, q.Hv},
+        {p->dq_strides, unit, grads, q.Hk}, {p->dk_strides, unit, grads, q.Hk}, {p->dv_strides, unit, grads, q.Hv}};
+    for (const auto &a : arrays)
+        if (!strides_ok(a.s, a.unit, a.out, q.B, a.heads, q.L)) return PGF_ERR_INVALID_ARG;
+    if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
+    q.DK = q.dk <= 64 ? 64 : 128;
+    q.nseq = p->n_seqs ? p->n_seqs : q.B;
+    const int64_t col_blocks = cdiv(q.dv, 16) + q.DK / 16;      // an upper bound of the blocks of one head
+    if (step) {
+        if (p->pool < 0 || p->pool > kMaxLen) return PGF_ERR_INVALID_ARG;
+        if (q.B * q.Hv > kMaxBlocks / col_blocks) return PGF_ERR_UNSUPPORTED;
+        *out = q;
+        return PGF_OK;
+    }
+    q.chunks_per = cdiv(q.L, kC);
+    q.chunk_slots = p->n_seqs ? q.L / kC + p->n_seqs : q.B * q.chunks_per;
+    if (q.chunk_slots * q.Hv > kMaxBlocks / col_blocks || q.nseq * q.Hv > kMaxBlocks / col_blocks)
+        return PGF_ERR_UNSUPPORTED;
+    q.seg = p->seg_len > 0 ? p->seg_len : 0;
+    if (q.seg >= q.L) q.seg = 0;
+    q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
+    q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
+    const int64_t cell = q.Hv * q.dk * q.dv * 4, cell_tr = q.Hv * (int64_t)q.DK * q.DK * 4;
+    const int64_t kRecBytes = 1632 * 4;
+    const int64_t ns = q.seg ? q.seg_slots : 0, nc = grads ? q.chunk_slots : 0;
+    bool ok = section(&q.total, &q.rec, q.chunk_slots, q.Hv * kRecBytes);
+    ok = ok && section(&q.total, &q.segE, ns, cell) && section(&q.total, &q.tr, ns, cell_tr);
+    ok = ok && section(&q.total, &q.S, nc, cell) && section(&q.total, &q.dS, nc, cell);
+    ok = ok && section(&q.total, &q.u, nc, q.Hv * kC * q.dv * 4) && section(&q.total, &q.du, nc, q.Hv * kC * q.dv * 4);
+    ok = ok && section(&q.total, &q.dseg, grads ? ns : 0, cell);
+    if (!ok) return PGF_ERR_UNSUPPORTED;
+    q.total = std::max<size_t>(q.total, 256);
+    *out = q;
+    return PGF_OK;
+}
+
+}  // namespace gdr
+
+namespace qk {
+
+int make_plan(const pgf_qk_params *p, Plan *out, bool grads) {
+    if (!p || !out) return PGF_ERR_INVALID_ARG;
+    Plan q{};
+    q.B = p->batch; q.Hq = p->q_heads; q.Hk = p->k_heads; q.L = p->seqlen; q.d = p->d_head; q.rot = p->rot;
+    if (q.B < 1 || q.Hq < 0 || q.Hk < 0 || q.Hq + q.Hk < 1 || q.L < 0 || q.d < 1 || q.rot < 0)
+        return PGF_ERR_INVALID_ARG;
+    if (p->in_dtype != PGF_F32 && p->in_dtype != PGF_BF16) return PGF_ERR_INVALID_ARG;
+    if (p->norm < PGF_NORM_NONE || p->norm > PGF_NORM_RMS) return PGF_ERR_INVALID_ARG;
+    if (!(p->eps >= 0.0f)) return PGF_ERR_INVALID_ARG;
+    if (q.rot > q.d || (q.rot && !p->inv_freq)) return PGF_ERR_INVALID_ARG;
+    if (q.rot && p->positions && p->pos_bits != 32 && p->pos_bits != 64) return PGF_ERR_INVALID_ARG;
+    if (p->pos_stride < 0 || p->pos_stride > kMaxStride) return PGF_ERR_INVALID_ARG;
+    if (q.d % 8 || q.d > 512 || q.rot % 16) return PGF_ERR_UNSUPPORTED;
+    if (q.B > kMaxBatch || q.Hq > kMaxHeads || q.Hk > kMaxHeads || q.L > kMaxLen) return PGF_ERR_UNSUPPORTED;
+    const int64_t unit = p->in_dtype == PGF_BF16 ? 8 : 4;
+    const struct { const int64_t (&s)[3]; bool out; int64_t heads; } arrays[] = {
+        {p->q_strides, false, q.Hq}, {p->k_strides, false, q.Hk}, {p->q_out_strides, true, q.Hq},
+        {p->k_out_strides, true, q.Hk}, {p->dq_strides, false, q.Hq}, {p->dk_strides, false, q.Hk}};
+    for (const auto &a : arrays)
+        if (!strides_ok(a.s, unit, a.out, q.B, a.heads, q.L)) return PGF_ERR_INVALID_ARG;
+    if ((double)q.B * (double)(q.Hq + q.Hk) * (double)q.L * (double)q.d > 4e18) return PGF_ERR_UNSUPPORTED;
+    if ((double)q.B * (double)q.L > (double)kMaxBlocks) return PGF_ERR_UNSUPPORTED;
+    q.G = 1;
+    while (q.G * 8 < q.d) q.G *= 2;
+    // Blocks of the gradient kernel: enough to fill the GPU several times; each
+    // leaves one partial sum of the weights' gradients.
+    q.blocks = std::min<int64_t>(std::max<int64_t>(1, q.B * q.L), 2048);
+    q.total = grads && (p->w_q || p->w_k) ? (size_t)q.blocks * 2 * q.d * sizeof(float) : 0;
+    *out = q;
+    return PGF_OK;
+}
+
+}  // namespace qk
+}  // namespace pgf
+
+extern "C" size_t pgf_gdr_workspace_bytes(const pgf_gdr_params *p) {
+    pgf::gdr::Plan q;
+    return pgf::gdr::make_plan(p, &q, p && p->grads, false) == PGF_OK ? q.total : 0;
+}
+
+extern "C" int pgf_gdr_plan(const pgf_gdr_params *p, int32_t *seg_len) {
+    if (!seg_len) return PGF_ERR_INVALID_ARG;
+    pgf::gdr::Plan q;
+    const int rc = pgf::gdr::make_plan(p, &q, p && p->grads, false);
+    if (rc == PGF_OK) *seg_len = (int32_t)q.seg;
+    return rc;
+}
+
+extern "C" size_t pgf_qk_norm_workspace_bytes(const pgf_qk_params *p) {
+    pgf::qk::Plan q;
+    return pgf::qk::make_plan(p, &q, true) == PGF_OK ? q.total : 0;
+}

@@ -1,0 +1,58 @@
+// Host-side planning of the gated delta rule and of the query/key
+// preparation: argument checks and workspace layout.  Plain C++ without
+// device access.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/pgf.h"
+
+namespace pgf {
+namespace gdr {
+
+constexpr int kC = 32;           // steps per chunk
+
+// Workspace sections (bytes, 256-byte aligned).
+//   rec   [chunk slots][Hv][kRec]             k_gdr_prep's record of each chunk
+//   seg   [segment slots][Hv][dk][dv]         zero-start end state of a segment,
+//                                             then (in place) its entry state
+//   tr    [segment slots][Hv][DK][DK]         transition of a segment
+// gradients:
+//   S     [chunk slots][Hv][dk][dv]           state entering each chunk
+//   dS    [chunk slots][Hv][dk][dv]           its adjoint leaving each chunk
+//   u, du [chunk slots][Hv][32][dv]           V' and dR of each chunk
+//   dseg  [segment slots][Hv][dk][dv]         as seg, of the adjoint
+struct Plan {
+    int64_t B, Hk, Hv, L, dk, dv, nseq;
+    int DK;                      // d_key padded to the kernels' 64 or 128
+    int64_t chunk_slots, chunks_per;     // slots of kC steps, of a dense sequence
+    int64_t seg;                 // steps per segment, 0 = sequences are not cut
+    int64_t seg_slots, segs_per;
+    size_t rec, segE, tr, S, dS, u, du, dseg, total;
+};
+
+// Validates sizes, types and strides, not pointers.  step: of pgf_gdr_step.
+int make_plan(const pgf_gdr_params *p, Plan *q, bool grads, bool step);
+
+}  // namespace gdr
+
+namespace qk {
+
+struct Plan {
+    int64_t B, Hq, Hk, L, d, rot;
+    int G;                       // lanes per head
+    int64_t blocks;              // blocks of the gradient kernel
+    size_t total;
+};
+int make_plan(const pgf_qk_params *p, Plan *q, bool grads);
+
+}  // namespace qk
+
+// Strides {0,0,0} stand for dense rows of `width` elements in [.., heads, L, width].
+void dense_strides(const int64_t (&in)[3], int64_t heads, int64_t L, int64_t width, int64_t (&out)[3]);
+// Bytes from the first to behind the last element of such an array (0 if empty).
+size_t extent(const int64_t (&s)[3], int64_t B, int64_t heads, int64_t L, int64_t width, size_t elem);
+bool overlaps(const void *a, size_t na, const void *b, size_t nb);
+
+}  // namespace pgf
