@@ -371,7 +371,8 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
  * gradients has strides in elements for batch, head and step ({0, 0, 0}: dense
  * row-major); the last index is dense.  A stride of zero broadcasts an input.
  * q, k, v, o and their gradients are f32 or bf16 (in_dtype); the arrays'
- * addresses and strides are multiples of 16 bytes (g and beta: of 4).
+ * addresses and strides are multiples of 16 bytes (g and beta: of 4), a step's
+ * stride below 2^24 bytes.
  *
  * Packed sequences: with n_seqs > 0, batch is 1 and the rows of the one
  * batch entry hold n_seqs sequences; sequence n has the rows cu_seqlens[n]

@@ -46,33 +46,118 @@ __device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t n) {
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(__bf16 x) { return (float)x; }
 
-template <typename T>
-struct Vec4 { T v[4]; };          // 4 consecutive elements, as loaded
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 
-__device__ __forceinline__ Vec4<float> load4(const float *p) {
-    const floatx4 x = *(const floatx4 *)p;
-    return {{x[0], x[1], x[2], x[3]}};
-}
-__device__ __forceinline__ Vec4<__bf16> load4(const __bf16 *p) {
-    const bf16x4 x = *(const bf16x4 *)p;
-    return {{x[0], x[1], x[2], x[3]}};
-}
-template <typename T>
-__device__ __forceinline__ Vec4<T> zero4() {
-    return {{(T)0.0f, (T)0.0f, (T)0.0f, (T)0.0f}};
+// A value that is the same in all lanes, held as such.
+__device__ __forceinline__ int64_t uni(int64_t x) {
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// bf16 numbers whose sum is x: P = 1 rounds (error 2^-9 relative), P = 2 leaves
-// 2^-18, P = 3 2^-27 (below an f32's own rounding).  For a bf16 input P = 1 is
-// exact.
+// Rows of one head from some step on, read and written through a buffer
+// descriptor: what lies behind the last live row reads as zero and is not
+// written, without a branch or a comparison.  A lane whose element is not
+// there gives the offset kNone.  The byte offset of row t is t * st; st is
+// below 2^24 (checked on the host), a chunk below 2^30.
+constexpr uint32_t kNone = 0x80000000u;
+struct Buf {
+    __amdgpu_buffer_rsrc_t r;
+    uint32_t st;                     // bytes from row to row
+};
+// `live` rows of `width` bytes at p, live >= 1
+__device__ __forceinline__ Buf make_buf(const void *p, uint32_t st, int live, int width) {
+    return Buf{__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)((uint32_t)(live - 1) * st + (uint32_t)width), 0x00020000), st};
+}
+// Element [b][h][t] of a view, as a base for make_buf (all arguments uniform).
+template <typename T>
+__device__ __forceinline__ const T *row_ptr(const View &v, int64_t b, int64_t h, int64_t t) {
+    return (const T *)uni((int64_t)(uintptr_t)v.at<const T>(b, h, t));
+}
+
+// Eight consecutive elements as they lie in memory: converted where they are
+// used, since a conversion waits for the load.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<__bf16> { uintx4 x; };
+template <>
+struct Raw8<float> { uintx4 x, y; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const Buf &b, uint32_t voff, uint32_t soff) {
+    Raw8<T> r;
+    r.x = __builtin_amdgcn_raw_buffer_load_b128(b.r, voff, soff, 0);
+    if constexpr (sizeof(T) == 4) r.y = __builtin_amdgcn_raw_buffer_load_b128(b.r, voff, soff + 16, 0);
+    return r;
+}
+// One element in a register of its own.
+template <typename T>
+__device__ __forceinline__ uint32_t load1(const Buf &b, uint32_t voff, uint32_t soff) {
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(b.r, voff, soff, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b32(b.r, voff, soff, 0);
+}
+template <typename T>
+__device__ __forceinline__ float raw_f(uint32_t u) { return __builtin_bit_cast(float, sizeof(T) == 2 ? u << 16 : u); }
+template <typename T>
+__device__ __forceinline__ void store1(const Buf &b, uint32_t voff, uint32_t soff, float x) {
+    if constexpr (sizeof(T) == 2)
+        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, (__bf16)x), b.r, voff, soff, 0);
+    else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), b.r, voff, soff, 0);
+}
+
+// Four consecutive elements.
+template <typename T>
+struct Raw4;
+template <>
+struct Raw4<float> {
+    floatx4 x;
+    __device__ __forceinline__ floatx4 f() const { return x; }
+};
+template <>
+struct Raw4<__bf16> {
+    bf16x4 x;
+    __device__ __forceinline__ floatx4 f() const { return __builtin_convertvector(x, floatx4); }
+};
+template <typename T>
+__device__ __forceinline__ Raw4<T> load4(const T *p) { return *(const Raw4<T> *)p; }
+template <typename T>
+__device__ __forceinline__ Raw4<T> zero4() {
+    Raw4<T> r;
+    r.x = {};
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ T *at_off(T *base, uint32_t bytes) { return (T *)((char *)base + (size_t)bytes); }
+
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two f32 as sums of P bf16 numbers each, o[i] the i-th numbers of both: P = 1
+// rounds (error 2^-9 relative), P = 2 leaves 2^-18, P = 3 2^-27 (below an f32's
+// own rounding).  For bf16 inputs P = 1 is exact.  In pairs, as the conversion
+// instruction takes them: 11 instructions for three parts of two numbers.
 template <int P>
-__device__ __forceinline__ void split(float x, __bf16 (&o)[P]) {
-    o[0] = (__bf16)x;
-    if constexpr (P > 1) {
-        const float r = x - (float)o[0];
-        o[1] = (__bf16)r;
-        if constexpr (P > 2) o[2] = (__bf16)(r - (float)o[1]);
+__device__ __forceinline__ void split2(floatx2 x, bf16x2 (&o)[P]) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+        o[i] = __builtin_convertvector(x, bf16x2);
+        if (i + 1 < P) {
+            const uint32_t u = __builtin_bit_cast(uint32_t, o[i]);
+            x[0] -= __builtin_bit_cast(float, u << 16);
+            x[1] -= __builtin_bit_cast(float, u & 0xffff0000u);
+        }
     }
+}
+
+// Four numbers' parts.
+template <int P>
+__device__ __forceinline__ void split4(const floatx4 &x, bf16x4 (&o)[P]) {
+    bf16x2 a[P], b[P];
+    split2<P>(floatx2{x[0], x[1]}, a);
+    split2<P>(floatx2{x[2], x[3]}, b);
+#pragma unroll
+    for (int i = 0; i < P; ++i) o[i] = __builtin_shufflevector(a[i], b[i], 0, 1, 2, 3);
 }
 
 template <int P>
@@ -83,33 +168,61 @@ struct Frag { bf16x8 p[P]; };
 template <int P>
 __device__ __forceinline__ Frag<P> to_frag(const floatx4 &lo, const floatx4 &hi) {
     Frag<P> f;
+    bf16x4 a[P], b[P];
+    split4<P>(lo, a);
+    split4<P>(hi, b);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        __bf16 a[P], b[P];
-        split<P>(lo[j], a);
-        split<P>(hi[j], b);
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            f.p[i][j] = a[i];
-            f.p[i][4 + j] = b[i];
-        }
-    }
+    for (int i = 0; i < P; ++i) f.p[i] = __builtin_shufflevector(a[i], b[i], 0, 1, 2, 3, 4, 5, 6, 7);
     return f;
+}
+
+// Parts of eight loaded elements (a bf16's only part is itself).
+template <int P>
+__device__ __forceinline__ Frag<P> raw_frag(const Raw8<__bf16> &r) {
+    static_assert(P == 1, "");
+    Frag<P> f;
+    f.p[0] = __builtin_bit_cast(bf16x8, r.x);
+    return f;
+}
+template <int P>
+__device__ __forceinline__ Frag<P> raw_frag(const Raw8<float> &r) {
+    return to_frag<P>(__builtin_bit_cast(floatx4, r.x), __builtin_bit_cast(floatx4, r.y));
 }
 
 // v_mfma_f32_16x16x32_bf16: lane (q, c) = (l / 16, l % 16) supplies eight
 // elements of row c of A and of column c of B, the same eight contraction
-// indexes in both, and receives D[4q + r][c].  Which index a slot stands for
-// is free as long as A and B agree.  Here slot (q, j) of a block of 32 is
-// index 4q + j (j < 4) or 16 + 4q + j - 4, so that two accumulator tiles are
-// a B operand as they lie; in memory a row is stored in slot order
-// (perm32 below), so that an A operand is one 16-byte read.
+// indexes in both (its "slots"), and receives D[4q + r][c].  Which index a slot
+// stands for is free as long as A and B agree, and so is the key that a row of
+// the state's tiles stands for:
+//   keys   tile 2 i + h, row 4 q + j is key 32 i + 8 q + 4 h + j, so slot 4 h + j
+//          of quad q is key 8 q + 4 h + j: two tiles are, as they lie, the B
+//          operand of products with K's rows in their natural order
+//   steps  tile h, row 4 q + j is step 16 h + 4 q + j, slot 4 h + j of quad q: two
+//          tiles are the B operand as they lie; T and A are stored in slot
+//          order (perm32), K by key is read by the transposing LDS read, four
+//          steps at a time
 __device__ __forceinline__ floatx4 mfma(const bf16x8 &a, const bf16x8 &b, const floatx4 &c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-
-// Position of index i of a block of 32 in slot order.
+// Position of step i of a chunk in slot order.
 __device__ __forceinline__ constexpr int perm32(int i) { return (i & 15) / 4 * 8 + (i >> 4) * 4 + (i & 3); }
+
+// Byte offset of 16-byte unit u of a row in LDS.  Rows are not padded; the
+// units of a row are permuted by an exclusive or with the row's number so that
+// the same unit of 16 rows spreads over all banks.  Rows of DK bf16, and of 32.
+template <int DK>
+__device__ __forceinline__ constexpr uint32_t unit_off(int row, int u) {
+    return (uint32_t)(row * (DK * 2) + ((u ^ (DK == 128 ? row & 15 : DK == 64 ? row >> 1 & 7 : row >> 2 & 3)) << 4));
+}
+
+// Rows t0 + 0..3 of four columns each, transposed by the read: lane i of 16
+// gives the address of row i / 4's columns 4 (i % 4).. and receives column i of the
+// four rows.
+__device__ __forceinline__ bf16x4 read_tr(const void *p) {
+    typedef short shortx4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                          (__attribute__((address_space(3))) shortx4 *)p));
+}
 
 // c + A B with A = sum of PA, B = sum of PB numbers; products below the
 // smallest kept part of either are left out (3 and 3 parts: 6 products).
@@ -169,10 +282,12 @@ struct Seqs {
     }
 };
 
-// Floats of a chunk's record (k_gdr_prep): T and A as three 16 x 16 blocks
-// each ((0,0), (1,0), (1,1), row-major), then e^G, e^{G_end - G} and beta of
-// its 32 steps.
-constexpr int kRecT = 0, kRecA = 768, kRecRow = 1536, kRec = 1632;
+// A chunk's record (k_gdr_prep), bytes: images of LDS arrays [32][32] of bf16
+// (2 KB each, unit_off<32>, columns in slot order): three parts of TW, PO of TA,
+// then e^G of the 32 steps, and for the gradients three parts of T^.
+constexpr uint32_t kImg = 2048;
+__host__ __device__ constexpr uint32_t rec_rows(int po) { return (3 + po) * kImg; }
+__host__ __device__ constexpr uint32_t rec_bytes(int po, bool grads) { return rec_rows(po) + 256 + (grads ? 3 * kImg : 0); }
 
 }  // namespace gdr
 }  // namespace pgf

@@ -1,0 +1,536 @@
+// Kernels shared by the scan and the gradients of the gated delta rule: the
+// chunks' records and the forward chain (see pgf_gdr.hip for the chunk form).
+#pragma once
+
+#include "pgf_gdr.h"
+
+namespace pgf {
+namespace gdr {
+
+struct Args {
+    View q, k, v, g, beta, o;
+    Seqs seqs;
+    int64_t chunk_per, seg_per, seg;     // (Seqs::of)
+    int Hk, Hv, rep, dk, dv;             // rep: value heads per key head
+    float scale;
+    char *rec;                           // [chunk slots][Hv] records
+    int grads;                           // the records hold T^ too
+    const float *S_in;                   // entry states per sequence (NULL = zero), or
+    const float *seg_in;                 // per segment
+    float *S_out;
+    float *segE, *tr;                    // kSegment: end states and transitions
+    float *saveS, *saveE;                // kSave: states entering every save-th chunk, E of every chunk
+    int64_t save_per; int save;          // slots of kC * save steps of a dense sequence
+    int ct, vt;                          // column tiles of a head, value tiles among them
+};
+
+// ---------------------------------------------------------------- prep
+// One wave per chunk and key head: K K^T and Q K^T once, then T^, TW and TA of
+// each of its value heads.  G and its differences are f64: a difference of two
+// long sums would lose the decay between neighbours.  T^ by 16 x 16 blocks: the
+// diagonal ones by substitution, one column a lane, the third is -T11 (N10 T00)
+// on the f32 matrix cores, as are the products of TA.  A decay below e^-200 a
+// step is zero in f32, as is e^-200, so -inf (forget everything) is taken as
+// -200 and no difference becomes inf - inf.
+// Bound by memory: it reads q and k once and writes the records (10 KB a chunk
+// and head in bf16).
+constexpr int kPrepWaves = 4;
+
+// Store at a 32-bit offset from a base that is the same for the whole wave.
+template <typename V>
+__device__ __forceinline__ void put(char *base, uint32_t bytes, const V &x) { *(V *)(base + (size_t)bytes) = x; }
+
+__device__ __forceinline__ floatx4 mfma_f32(float a, float b, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+template <typename T, int DK>
+__global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu(3))) void k_gdr_prep(Args a, int64_t slots) {
+    constexpr int P = sizeof(T) == 2 ? 1 : 3, PO = sizeof(T) == 2 ? 2 : 3, KS = DK / 32;
+    struct Lds {
+        __align__(16) float D[2][16][20];     // diagonal blocks of N diag(beta), by column
+        __align__(16) float L10[16][20];
+        __align__(16) float Ti[3][16][20];     // T^: blocks (0,0), (1,0), (1,1)
+        __align__(16) float A[3][16][20];     // A diag(beta)
+        __align__(16) double G[32];
+        __align__(16) float be[32];
+    };
+    __shared__ Lds lds[kPrepWaves];
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int lane = threadIdx.x % 64, c = lane % 16, qd = lane / 16;
+    Lds &s = lds[w];
+    const int64_t item = (int64_t)blockIdx.x * kPrepWaves + w;
+    if (item >= slots * a.Hk) return;
+    const int64_t slot = item / a.Hk;
+    const int hk = (int)(item - slot * a.Hk);
+    const Rows r = a.seqs.of(slot, kC, a.chunk_per);
+    if (r.unit0 >= r.len) return;
+    const int live = (int)uni(r.len - r.unit0 < kC ? r.len - r.unit0 : kC);
+    const int64_t t0 = r.lo + r.unit0;
+
+    floatx4 kk[3], qk[3];                // blocks (0,0), (1,0), (1,1)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) kk[i] = qk[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    {
+        const Buf kb = make_buf(row_ptr<T>(a.k, r.b, hk, t0), (uint32_t)a.k.st * sizeof(T), live, a.dk * (int)sizeof(T));
+        const Buf qb = make_buf(row_ptr<T>(a.q, r.b, hk, t0), (uint32_t)a.q.st * sizeof(T), live, a.dk * (int)sizeof(T));
+        Raw8<T> kx[KS][2], qx[KS][2];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const uint32_t e = 32 * ks + 8 * qd;
+                const bool on = (int)e < a.dk;
+                kx[ks][m] = load8<T>(kb, on ? (16 * m + c) * kb.st + e * sizeof(T) : kNone, 0);
+                qx[ks][m] = load8<T>(qb, on ? (16 * m + c) * qb.st + e * sizeof(T) : kNone, 0);
+            }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag<P> kf[2], qf[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                kf[m] = raw_frag<P>(kx[ks][m]);
+                qf[m] = raw_frag<P>(qx[ks][m]);
+            }
+            kk[0] = mfma_parts<P, P>(kf[0], kf[0], kk[0]);
+            kk[1] = mfma_parts<P, P>(kf[1], kf[0], kk[1]);
+            kk[2] = mfma_parts<P, P>(kf[1], kf[1], kk[2]);
+            qk[0] = mfma_parts<P, P>(qf[0], kf[0], qk[0]);
+            qk[1] = mfma_parts<P, P>(qf[1], kf[0], qk[1]);
+            qk[2] = mfma_parts<P, P>(qf[1], kf[1], qk[2]);
+        }
+    }
+    const uint32_t rb = rec_bytes(PO, a.grads);
+    for (int vh = 0; vh < a.rep; ++vh) {
+        const int h = hk * a.rep + vh;
+        char *rec = (char *)uni((int64_t)(uintptr_t)(a.rec + (slot * a.Hv + h) * (int64_t)rb));
+        const int t = lane % 32;
+        float g = 0.0f, be = 0.0f;
+        if (t < live) {
+            g = *a.g.at<const float>(r.b, h, t0 + t);
+            be = *a.beta.at<const float>(r.b, h, t0 + t);
+            g = g < -200.0f ? -200.0f : g;
+        }
+        double G = g;
+#pragma unroll
+        for (int m = 1; m < 32; m *= 2) {
+            const double o = __shfl_up(G, m, 32);
+            if (t >= m) G += o;
+        }
+        const double Gend = __shfl(G, 31, 32);
+        wave_lds();
+        s.G[t] = G;                      // (the upper lanes repeat the lower ones)
+        s.be[t] = be;
+        put(rec, rec_rows(PO) + 4 * t, expf((float)G));
+        wave_lds();
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const int bm = i > 0, bn = i > 1;
+            const double Gs = s.G[16 * bn + c];
+            const float bs = s.be[16 * bn + c];
+            floatx4 nb;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 4 * qd + j;
+                const bool on = bm != bn || row >= c, below = bm != bn || row > c;
+                const float dG = (float)(s.G[16 * bm + row] - Gs);
+                const float d = expf(on ? dG : 0.0f) * bs;
+                s.A[i][row][c] = on ? d * qk[i][j] : 0.0f;
+                nb[j] = below ? d * kk[i][j] : 0.0f;
+                if (i == 1) s.L10[row][c] = nb[j];
+            }
+            if (i != 1) *(floatx4 *)&s.D[bn][c][4 * qd] = nb;
+        }
+        wave_lds();
+        // column c of diagonal block qd & 1 (the upper lanes repeat the lower
+        // ones): once an entry is known it leaves the rows below it
+        const int bd = qd & 1;
+        float tc[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) tc[i] = i == c ? 1.0f : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 15; ++j) {
+#pragma unroll
+            for (int i4 = j / 4 * 4; i4 < 16; i4 += 4) {
+                const floatx4 l = *(const floatx4 *)&s.D[bd][j][i4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i4 + i > j) tc[i4 + i] = fmaf(-l[i], tc[j], tc[i4 + i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);     // one column's reads at a time, or all take registers
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s.Ti[2 * bd][i][c] = tc[i];
+        wave_lds();
+        floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f}, t10 = x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)      // N10 T00; contraction index 4 j + qd
+            x = mfma_f32(s.L10[c][4 * j + qd], s.Ti[0][4 * j + qd][c], x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)      // T11 x; contraction index 4 qd + j, as x lies
+            t10 = mfma_f32(s.Ti[2][c][4 * qd + j], x[j], t10);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s.Ti[1][4 * qd + j][c] = -t10[j];
+        wave_lds();
+        // TA by transposed products, so that a lane receives four columns of a
+        // row: row c, columns 4 qd .. 4 qd + 3 of each block
+        floatx4 ta[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) ta[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int k = 4 * j + qd;
+            const float a00 = s.A[0][c][k], a10 = s.A[1][c][k], a11 = s.A[2][c][k];
+            const float t00 = s.Ti[0][k][c], t10_ = s.Ti[1][k][c], t11 = s.Ti[2][k][c];
+            ta[0] = mfma_f32(t00, a00, ta[0]);
+            ta[1] = mfma_f32(t00, a10, ta[1]);
+            ta[1] = mfma_f32(t10_, a11, ta[1]);
+            ta[2] = mfma_f32(t11, a11, ta[2]);
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const int bm = i > 0, bn = i > 1, row = 16 * bm + c;
+            const uint32_t at = unit_off<32>(row, qd) + 8 * bn;
+            const floatx4 tr = *(const floatx4 *)&s.Ti[i][c][4 * qd];
+            const float ob = expf((float)(Gend - s.G[row])) * s.be[row];
+            bf16x4 o[3], u[PO];
+            split4<3>(floatx4{tr[0] * ob, tr[1] * ob, tr[2] * ob, tr[3] * ob}, o);
+            split4<PO>(ta[i], u);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) put(rec, p * kImg + at, o[p]);
+#pragma unroll
+            for (int p = 0; p < PO; ++p) put(rec, (3 + p) * kImg + at, u[p]);
+            if (a.grads) {
+                split4<3>(tr, o);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) put(rec, rec_rows(PO) + 256 + p * kImg + at, o[p]);
+            }
+        }
+        // block (0,1)
+        const uint32_t at = unit_off<32>(c, qd) + 8;
+        const bf16x4 zero = {};
+#pragma unroll
+        for (int p = 0; p < 3 + PO; ++p) put(rec, p * kImg + at, zero);
+        if (a.grads) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) put(rec, rec_rows(PO) + 256 + p * kImg + at, zero);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- chain
+// A wave owns 16 columns of the state of one head, all its keys, in
+// accumulators, and takes its segment chunk by chunk; the waves of a block
+// share the chunk's keys, queries, TW and TA in LDS.  Every product contracts
+// over the rows of the wave's own last result, which lies as the operand it is
+// needed as (see mfma), so nothing crosses waves but the staged chunk; the
+// next one is loaded into registers meanwhile.
+//   kOut      outputs, from the true entry state
+//   kSegment  zero-start end state of the segment (value columns) and its
+//             transition (columns of the identity, v = 0)
+//   kSave     for the gradients: E of every chunk and the state entering every
+//             save-th one
+enum Mode { kOut, kSegment, kSave };
+
+template <typename T, int DK, int MODE>
+struct Chunk {
+    static constexpr int P = sizeof(T) == 2 ? 1 : 3;      // parts of q and k
+    static constexpr int PO = sizeof(T) == 2 ? 2 : 3;     // parts of f32 operands of the output alone
+    static constexpr int NI = MODE == kOut ? 3 + PO : MODE == kSave ? 6 : 3;   // images: TW, then TA or T^
+    __align__(16) char K[P][32 * DK * 2];
+    __align__(16) char Q[MODE == kOut ? P : 1][MODE == kOut ? 32 * DK * 2 : 16];
+    __align__(16) char M[NI][kImg];
+    __align__(16) float eG[32];
+};
+
+template <typename T, int DK, int MODE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_chain(Args a, uint32_t n_items) {
+    using Ck = Chunk<T, DK, MODE>;
+    constexpr int P = Ck::P, PO = Ck::PO, NI = Ck::NI;
+    constexpr bool OUT = MODE == kOut;
+    constexpr int KS = DK / 32, KT = DK / 16;
+    constexpr int KU = 32 * DK / 8 / 256;          // 8-key units of K a thread stages (and of Q)
+    constexpr int MU = (NI * 128 + 255) / 256;     // 16-byte units of the images
+    // Two chunks in LDS where a CU still holds two blocks (one barrier a chunk).
+    constexpr int NB = sizeof(Ck) <= 40960 ? 2 : 1;
+    __shared__ Ck lds[NB];
+    const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int cb = (a.ct + 3) / 4;                 // blocks of a head
+    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const int64_t sh = item / cb;
+    const int tile = (int)(item - sh * cb) * 4 + w;
+    const int64_t slot = sh / a.Hv;
+    const int h = (int)(sh - slot * a.Hv), hk = h / a.rep;
+    const Rows r = a.seqs.of(slot, a.seg ? a.seg : a.seqs.L + 1, a.seg_per);
+    // A slot behind its sequence's end has no steps; a sequence of none still
+    // hands its state on (its first slot).
+    if (r.unit0 > 0 && r.unit0 >= r.len) return;   // uniform over the block
+    int64_t n = uni(r.len - r.unit0);
+    if (a.seg && n > a.seg) n = a.seg;
+    const bool last = r.unit0 + n >= r.len;
+    const bool value = tile < a.vt, mine = tile < a.ct;
+    const int col = (value ? tile : tile - a.vt) * 16 + c;
+    const bool live_col = mine && (value ? col < a.dv : col < a.dk);
+    const int chunks = (int)((n + kC - 1) / kC);
+    const int64_t t0 = r.lo + r.unit0;
+    const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
+
+    const int64_t save0 =
+        MODE == kSave ? uni(a.seqs.slot0(r.n, kC * a.save, a.save_per) + r.unit0 / (kC * a.save)) : 0;
+
+    // S[kt][j]: key key0(kt) + j of this lane's column
+    auto key0 = [&](int kt) { return 32 * (kt / 2) + 8 * qd + 4 * (kt & 1); };
+    floatx4 S[KT];
+    {
+        const float *in = MODE == kSegment ? nullptr : a.seg_in ? a.seg_in + (slot * a.Hv + h) * a.dk * a.dv
+                          : a.S_in ? a.S_in + (r.n * a.Hv + h) * a.dk * a.dv : nullptr;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (in) {                                  // (loads without conditions: a branch around one waits for it)
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const bool on = live_col && key0(kt) < a.dk;       // d_key is a multiple of 8
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    S[kt][j] = *at_off(in, (uint32_t)(on ? (key0(kt) + j) * a.dv + col : 0) * 4u);
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+                if (!(live_col && key0(kt) < a.dk)) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        if (MODE == kSegment && !value) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[kt][j] = key0(kt) + j == col ? 1.0f : 0.0f;
+        }
+    }
+    auto store_state = [&](float *out, int ld) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+            if (live_col && key0(kt) < a.dk) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *at_off(out, (uint32_t)((key0(kt) + j) * ld + col) * 4u) = S[kt][j];
+            }
+    };
+
+    // What this thread stages of a chunk.  Rows behind the sequence's end read
+    // as zero; their beta is zero in the record, so they write nothing.
+    Raw8<T> rk[KU], rq[OUT ? KU : 1];
+    uintx4 rm[MU];
+    float reG;
+    uint32_t rv[2][4];
+    const T *kp = row_ptr<T>(a.k, r.b, hk, t0), *qp = row_ptr<T>(a.q, r.b, hk, t0), *vp = row_ptr<T>(a.v, r.b, h, t0),
+            *op = row_ptr<T>(a.o, r.b, h, t0);
+    const uint32_t vst = (uint32_t)a.v.st * sizeof(T), ost = (uint32_t)a.o.st * sizeof(T);
+    const uint32_t vo = live_col && value ? 4 * qd * vst + col * (uint32_t)sizeof(T) : kNone;
+    const uint32_t oo = live_col ? 4 * qd * ost + col * (uint32_t)sizeof(T) : kNone;
+    const uint32_t kst = (uint32_t)a.k.st * sizeof(T), qst = (uint32_t)a.q.st * sizeof(T);
+    const uint32_t rb = rec_bytes(PO, MODE == kSave);
+    uint32_t ko[KU], qo[KU];
+#pragma unroll
+    for (int i = 0; i < KU; ++i) {
+        const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
+        ko[i] = e < a.dk ? t * kst + e * (uint32_t)sizeof(T) : kNone;
+        qo[i] = e < a.dk ? t * qst + e * (uint32_t)sizeof(T) : kNone;
+    }
+    auto live_rows = [&](int ch) {
+        const int64_t left = n - (int64_t)ch * kC;
+        return (int)(left < kC ? left : kC);
+    };
+    auto fetch = [&](int ch) {
+        const int live = live_rows(ch);
+        const Buf kb = make_buf(kp + (int64_t)ch * kC * a.k.st, kst, live, a.dk * (int)sizeof(T));
+        const Buf qb = make_buf(qp + (int64_t)ch * kC * a.q.st, qst, live, a.dk * (int)sizeof(T));
+        const Buf vb = make_buf(vp + (int64_t)ch * kC * a.v.st, vst, live, a.dv * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            rk[i] = load8<T>(kb, ko[i], 0);
+            if constexpr (OUT) rq[i] = load8<T>(qb, qo[i], 0);
+        }
+        const char *rec = a.rec + ((slot0 + ch) * a.Hv + h) * (int64_t)rb;
+#pragma unroll
+        for (int i = 0; i < MU; ++i) {
+            const int u = tid + 256 * i < NI * 128 ? tid + 256 * i : tid;
+            rm[i] = *(const uintx4 *)(rec + (MODE == kSave && u >= 384 ? rec_rows(PO) + 256 - 384 * 16 : 0u) + 16u * u);
+        }
+        reG = *(const float *)(rec + rec_rows(PO) + 4 * (tid % 32));
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) rv[m][j] = load1<T>(vb, vo, (16 * m + j) * vst);
+    };
+    auto stage = [&](Ck &s) {
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int u = tid + 256 * i, t = u / (DK / 8);
+            const uint32_t at = unit_off<DK>(t, u % (DK / 8));
+            const Frag<P> f = raw_frag<P>(rk[i]);
+#pragma unroll
+            for (int p = 0; p < P; ++p) *(bf16x8 *)&s.K[p][at] = f.p[p];
+            if constexpr (OUT) {
+                const Frag<P> y = raw_frag<P>(rq[i]);
+#pragma unroll
+                for (int p = 0; p < P; ++p) *(bf16x8 *)&s.Q[p][at] = y.p[p];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MU; ++i)
+            if (64 * w + 256 * i < NI * 128) *(uintx4 *)(&s.M[0][0] + 16 * (tid + 256 * i)) = rm[i];
+        if (tid < 32) s.eG[tid] = reG;
+    };
+
+    if (chunks > 0) {
+        fetch(0);
+        stage(lds[0]);
+        lds_barrier();
+    }
+    for (int ch = 0; ch < chunks; ++ch) {
+        if constexpr (MODE == kSave)
+            if (mine && ch % a.save == 0)
+                store_state(a.saveS + ((save0 + ch / a.save) * a.Hv + h) * a.dk * a.dv, a.dv);
+        float vv[2][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) vv[m][j] = raw_f<T>(rv[m][j]);
+        const Ck &s = lds[NB == 2 ? ch & 1 : 0];
+        fetch(ch + 1 < chunks ? ch + 1 : ch);      // (the last chunk again rather than a branch)
+        if (mine) {
+            // Operands are read a step ahead of their products: left to
+            // itself the compiler reads each where it is needed and waits.
+            floatx4 kS[2], qS[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) kS[m] = qS[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            Frag<P> kf[2][2], qf[2][2];
+            auto read_kq = [&](int ks) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const uint32_t at = unit_off<DK>(16 * m + c, 4 * ks + qd);
+                        kf[ks & 1][m].p[p] = *(const bf16x8 *)&s.K[p][at];
+                        if constexpr (OUT) qf[ks & 1][m].p[p] = *(const bf16x8 *)&s.Q[p][at];
+                    }
+            };
+            Frag<3> tf[2];
+            floatx4 eG[2];
+            read_kq(0);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 1 < KS) read_kq(ks + 1);
+                else {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                        for (int p = 0; p < 3; ++p)
+                            tf[m].p[p] = *(const bf16x8 *)&s.M[p][unit_off<32>(16 * m + c, qd)];
+                        eG[m] = *(const floatx4 *)&s.eG[16 * m + 4 * qd];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                const Frag<3> sp = to_frag<3>(S[2 * ks], S[2 * ks + 1]);
+                Frag<PO> so;
+#pragma unroll
+                for (int p = 0; p < PO; ++p) so.p[p] = sp.p[p];
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    kS[m] = mfma_parts<P, 3>(kf[ks & 1][m], sp, kS[m]);
+                    if constexpr (OUT) qS[m] = mfma_parts<P, PO>(qf[ks & 1][m], so, qS[m]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            floatx4 X[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    X[m][j] = fmaf(-eG[m][j], kS[m][j], vv[m][j]);
+                    if constexpr (OUT) qS[m][j] *= eG[m][j];
+                }
+            const Frag<3> xp = to_frag<3>(X[0], X[1]);
+            constexpr int GK = P == 1 ? 4 : 2;     // key tiles read at a time
+            Frag<P> ktf[2][GK];
+            auto read_kt = [&](int g) {
+#pragma unroll
+                for (int i = 0; i < GK; ++i) {
+                    const int kt = g * GK + i, row = 4 * qd + c / 4;
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        const char *k0 = &s.K[p][unit_off<DK>(row, 4 * (kt / 2) + c % 4) + 8 * (kt & 1)];
+                        const char *k1 = &s.K[p][unit_off<DK>(16 + row, 4 * (kt / 2) + c % 4) + 8 * (kt & 1)];
+                        ktf[g & 1][i].p[p] = __builtin_shufflevector(read_tr(k0), read_tr(k1), 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
+                }
+            };
+            read_kt(0);
+            const float end = s.eG[31];
+            __builtin_amdgcn_sched_barrier(0);
+            floatx4 W[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) W[m] = mfma_parts<3, 3>(tf[m], xp, floatx4{0.0f, 0.0f, 0.0f, 0.0f});
+            const Frag<3> wp = to_frag<3>(W[0], W[1]);
+            Frag<MODE == kOut ? PO : 3> af[2];
+            if constexpr (MODE != kSegment) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int p = 0; p < NI - 3; ++p)
+                        af[m].p[p] = *(const bf16x8 *)&s.M[3 + p][unit_off<32>(16 * m + c, qd)];
+            }
+#pragma unroll
+            for (int g = 0; g < KT / GK; ++g) {
+                if (g + 1 < KT / GK) read_kt(g + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < GK; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[g * GK + i][j] *= end;
+                // part by part over the tiles, so that no product waits for the last one
+#pragma unroll
+                for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        if (sum - p >= 0)
+#pragma unroll
+                            for (int i = 0; i < GK; ++i)
+                                S[g * GK + i] = mfma(ktf[g & 1][i].p[p], wp.p[sum - p], S[g * GK + i]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (OUT) {
+                Frag<PO> xo;
+#pragma unroll
+                for (int p = 0; p < PO; ++p) xo.p[p] = xp.p[p];
+                const Buf ob = make_buf(op + (int64_t)ch * kC * a.o.st, ost, live_rows(ch), a.dv * (int)sizeof(T));
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const floatx4 o = mfma_parts<PO, PO>(af[m], xo, qS[m]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * m + j) * ost, o[j] * a.scale);
+                }
+            }
+            if constexpr (MODE == kSave) {
+                float *eb = a.saveE + ((slot0 + ch) * a.Hv + h) * (int64_t)(kC * a.dv);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const floatx4 e = mfma_parts<3, 3>(af[m], xp, floatx4{0.0f, 0.0f, 0.0f, 0.0f});
+                    if (live_col) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) *at_off(eb, (uint32_t)((16 * m + 4 * qd + j) * a.dv + col) * 4u) = e[j];
+                    }
+                }
+            }
+        }
+        if constexpr (NB == 1) lds_barrier();
+        stage(lds[NB == 2 ? (ch + 1) & 1 : 0]);
+        lds_barrier();
+    }
+    if (!mine) return;
+    if constexpr (MODE == kSegment)
+        store_state(value ? a.segE + (slot * a.Hv + h) * a.dk * a.dv : a.tr + (slot * a.Hv + h) * DK * DK, value ? a.dv : DK);
+    else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv, a.dv);
+}
+
+}  // namespace gdr
+}  // namespace pgf

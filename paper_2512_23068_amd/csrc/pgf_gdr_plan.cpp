@@ -11,6 +11,7 @@ namespace {
 constexpr int64_t kMaxBlocks = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxHeads = int64_t(1) << 16, kMaxBatch = int64_t(1) << 24, kMaxLen = int64_t(1) << 32;
 constexpr int64_t kMaxStride = int64_t(1) << 44;
+constexpr int64_t kMaxStep = (int64_t(1) << 24) - 16;      // bytes from step to step
 constexpr size_t kMaxTotal = size_t(1) << 46;
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -78,6 +79,8 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
         {p->dq_strides, unit, grads, q.Hk}, {p->dk_strides, unit, grads, q.Hk}, {p->dv_strides, unit, grads, q.Hv}};
     for (const auto &a : arrays)
         if (!strides_ok(a.s, a.unit, a.out, q.B, a.heads, q.L)) return PGF_ERR_INVALID_ARG;
+    for (const auto &a : arrays)
+        if (a.s[2] * 16 / unit > kMaxStep) return PGF_ERR_UNSUPPORTED;
     if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
     q.DK = q.dk <= 64 ? 64 : 128;
     q.nseq = p->n_seqs ? p->n_seqs : q.B;
@@ -97,9 +100,9 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
     q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
     const int64_t cell = q.Hv * q.dk * q.dv * 4, cell_tr = q.Hv * (int64_t)q.DK * q.DK * 4;
-    const int64_t kRecBytes = 1632 * 4;
+    q.rec_bytes = kImgBytes * (p->in_dtype == PGF_BF16 ? 5 : 6) + 256 + (grads ? 3 * kImgBytes : 0);
     const int64_t ns = q.seg ? q.seg_slots : 0, nc = grads ? q.chunk_slots : 0;
-    bool ok = section(&q.total, &q.rec, q.chunk_slots, q.Hv * kRecBytes);
+    bool ok = section(&q.total, &q.rec, q.chunk_slots, q.Hv * q.rec_bytes);
     ok = ok && section(&q.total, &q.segE, ns, cell) && section(&q.total, &q.tr, ns, cell_tr);
     ok = ok && section(&q.total, &q.S, nc, cell) && section(&q.total, &q.dS, nc, cell);
     ok = ok && section(&q.total, &q.u, nc, q.Hv * kC * q.dv * 4) && section(&q.total, &q.du, nc, q.Hv * kC * q.dv * 4);

@@ -12,9 +12,10 @@ namespace pgf {
 namespace gdr {
 
 constexpr int kC = 32;           // steps per chunk
+constexpr int64_t kImgBytes = 2048;  // a 32 x 32 matrix of bf16
 
 // Workspace sections (bytes, 256-byte aligned).
-//   rec   [chunk slots][Hv][kRec]             k_gdr_prep's record of each chunk
+//   rec   [chunk slots][Hv]                   k_gdr_prep's record of each chunk
 //   seg   [segment slots][Hv][dk][dv]         zero-start end state of a segment,
 //                                             then (in place) its entry state
 //   tr    [segment slots][Hv][DK][DK]         transition of a segment
@@ -29,6 +30,7 @@ struct Plan {
     int64_t chunk_slots, chunks_per;     // slots of kC steps, of a dense sequence
     int64_t seg;                 // steps per segment, 0 = sequences are not cut
     int64_t seg_slots, segs_per;
+    int64_t rec_bytes;           // of one chunk's record
     size_t rec, segE, tr, S, dS, u, du, dseg, total;
 };
 
