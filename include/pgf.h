@@ -397,7 +397,7 @@ typedef struct pgf_gdr_params {
     int32_t in_dtype;               /* PGF_F32 or PGF_BF16                        */
     /* Steps per segment: sequences are cut into segments whose transitions
      * are composed, so that they run side by side.  0 = library default, -1 =
-     * not cut, else a multiple of 32. */
+     * not cut, else a multiple of 64. */
     int32_t seg_len;
     float scale;
     int32_t grads;                  /* planning calls: 1 = of pgf_gdr_grads       */
@@ -433,6 +433,17 @@ int pgf_gdr_plan(const pgf_gdr_params *p, int32_t *seg_len);
  * workspace anything. */
 int pgf_gdr_scan(const void *q, const void *k, const void *v, const float *g, const float *beta,
                  const pgf_gdr_params *p, void *o, void *stream);
+
+/* The gradients of l for the adjoint signal do_ = dl/do (with o's shape and
+ * o_strides) and dl/dS_out (p->dS_out):
+ *   dq, dk [B, key_heads, L, d_key], dv [B, value_heads, L, d_value] in in_dtype
+ *   dg, dbeta [B, value_heads, L] (f32, dense row-major)
+ *   dl/dS_in into p->dS_in
+ * all overwritten; the gradients of a shared key head are summed over its
+ * value heads, in their order.  dq, dk and dv may be parts of one array's
+ * rows; no output may overlap an input. */
+int pgf_gdr_grads(const void *q, const void *k, const void *v, const float *g, const float *beta, const void *do_,
+                  const pgf_gdr_params *p, void *dq, void *dk, void *dv, float *dg, float *dbeta, void *stream);
 
 /* A few steps in place on a pool of states: entry b advances S_pool[slots[b]]
  * by its L steps (any L, made for one to a few) and writes its o.  An entry

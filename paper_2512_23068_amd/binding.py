@@ -98,7 +98,7 @@ class PgfPlanInfo(ctypes.Structure):
 EXPORTED = ("pgf_workspace_bytes", "pgf_plan", "pgf_scan_jvp", "pgf_scan_jvp_noalloc", "pgf_scan_jvp2",
             "pgf_param_grads",
             "pgf_la_workspace_bytes", "pgf_la_plan", "pgf_la_scan_jvp",
-            "pgf_gdr_workspace_bytes", "pgf_gdr_plan", "pgf_gdr_scan", "pgf_gdr_step",
+            "pgf_gdr_workspace_bytes", "pgf_gdr_plan", "pgf_gdr_scan", "pgf_gdr_grads", "pgf_gdr_step",
             "pgf_qk_norm_workspace_bytes", "pgf_qk_norm", "pgf_qk_norm_grads", "pgf_status_string", "pgf_timing_enable",
             "pgf_timing_read")
 
@@ -144,6 +144,8 @@ def lib():
     L.pgf_gdr_plan.argtypes = [GP, ctypes.POINTER(ctypes.c_int32)]
     L.pgf_gdr_scan.restype = ctypes.c_int
     L.pgf_gdr_scan.argtypes = [V] * 5 + [GP, V, V]
+    L.pgf_gdr_grads.restype = ctypes.c_int
+    L.pgf_gdr_grads.argtypes = [V] * 6 + [GP] + [V] * 6
     L.pgf_gdr_step.restype = ctypes.c_int
     L.pgf_gdr_step.argtypes = [V] * 5 + [GP, V, V]
     L.pgf_qk_norm_workspace_bytes.restype = ctypes.c_size_t
@@ -757,6 +759,55 @@ def gdr_scan(q, k, v, g, beta, *, scale=None, S_in=None, return_state=False, cu_
         _check(L_.pgf_gdr_scan(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), ctypes.byref(p), _ptr(o),
                                ctypes.c_void_p(st)))
         return (o, S_out) if return_state else o
+
+
+def gdr_grads(q, k, v, g, beta, do, *, scale=None, S_in=None, dS_out=None, cu_seqlens=None, seg_len=0, workspace=None,
+              out=None, stream=None):
+    """Gradients of the gated delta rule on the GPU for the adjoint signal
+    do = dl/do [B,Hv,L,dv] (in q's type) and dS_out = dl/dS_out (float32, None:
+    zero).
+
+    Inputs as in gdr_scan (of q and k after their preparation).  out: optional
+    (dq, dk, dv) outputs.  Returns (dq, dk, dv) in q's type, dg and dbeta
+    [B,Hv,L] float32, and with S_in or dS_out also dS_in (float32).  Gradients of
+    rows of no packed sequence are zero where the output is a new one.
+    """
+    _all_on_device(q, k, v, g, beta)
+    with torch.cuda.device(q.device), _on_stream(stream, q.device):
+        L_ = lib()
+        p, (q, k, v, g, beta) = _gdr_inputs(q, k, v, g, beta, scale, seg_len)
+        p.grads = 1
+        dev = q.device
+        B, Hv, L, dv = v.shape
+        do = _rows(do, v.shape, dev, "do", (q.dtype,))
+        _set_strides(p.o_strides, do)
+        n = _gdr_packed(p, cu_seqlens, B, dev)
+        cell = (n, Hv, q.shape[3], dv)
+        S_in, dS_out = _state(S_in, cell, dev, "S_in"), _state(dS_out, cell, dev, "dS_out")
+        p.S_in = None if S_in is None else S_in.data_ptr()
+        p.dS_out = None if dS_out is None else dS_out.data_ptr()
+        if out is None:
+            grads = [_like_rows(t, t.shape, q.dtype) for t in (q, k, v)]
+            if cu_seqlens is not None:
+                for t in grads:
+                    t.zero_()
+        else:
+            if len(out) != 3:
+                raise ValueError("out: expected (dq, dk, dv)")
+            grads = [_check_rows_out(o, t.shape, q.dtype, dev, f"out[{i}]") for i, (o, t) in enumerate(zip(out, (q, k, v)))]
+        for field, t in zip((p.dq_strides, p.dk_strides, p.dv_strides), grads):
+            _set_strides(field, t)
+        new = torch.empty if cu_seqlens is None else torch.zeros
+        dg, dbeta = (new((B, Hv, L), device=dev, dtype=torch.float32) for _ in range(2))
+        dS_in = None
+        if S_in is not None or dS_out is not None:
+            dS_in = torch.empty(cell, device=dev, dtype=torch.float32)
+            p.dS_in = dS_in.data_ptr()
+        workspace = _gdr_workspace(L_, p, workspace, dev)
+        st = torch.cuda.current_stream(dev).cuda_stream
+        _check(L_.pgf_gdr_grads(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(do), ctypes.byref(p),
+                                *[_ptr(t) for t in grads], _ptr(dg), _ptr(dbeta), ctypes.c_void_p(st)))
+        return (*grads, dg, dbeta) + (() if dS_in is None else (dS_in,))
 
 
 def gdr_step(q, k, v, g, beta, S, *, slots=None, scale=None, qk_prep=None, out=None, stream=None):

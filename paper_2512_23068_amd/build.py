@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 OUT = os.path.join(_HERE, "libpgf.so")
-SOURCES = ["pgf_scan.hip", "pgf_scan_f32.hip", "pgf_scan_bf16.hip", "pgf_la.hip", "pgf_gdr.hip", "pgf_qk.hip",
+SOURCES = ["pgf_scan.hip", "pgf_scan_f32.hip", "pgf_scan_bf16.hip", "pgf_la.hip", "pgf_gdr.hip", "pgf_gdr_grads.hip", "pgf_qk.hip",
            "pgf_plan.cpp", "pgf_gdr_plan.cpp", "pgf_timing.cpp",
            "pgf_stream.cpp"]
 # Packed FP32 instructions stay disabled in every HIP object of this library.

@@ -18,10 +18,17 @@ struct Args {
     const float *S_in;                   // entry states per sequence (NULL = zero), or
     const float *seg_in;                 // per segment
     float *S_out;
-    float *segE, *tr;                    // kSegment: end states and transitions
+    float *segE, *tr;                    // kSegment: end states, transitions (tr[j][i]: of entry (i, j))
     float *saveS, *saveE;                // kSave: states entering every save-th chunk, E of every chunk
     int64_t save_per; int save;          // slots of kC * save steps of a dense sequence
     int ct, vt;                          // column tiles of a head, value tiles among them
+    // gradients
+    View go, dq, dk_, dv_;               // dl/do; dl/dq, dl/dk, dl/dv
+    const float *dS_out, *dseg_in;       // dl/dS leaving sequences (NULL = zero), or segments
+    float *dS_in;                        // dl/dS entering sequences
+    float *dsegE;                        // kBackSegment: adjoint at the segments' starts, from zero
+    float *saveD, *saveU;                // kBack: adjoint of the state leaving every save chunks, dl/dE of every chunk
+    float *dg, *dbeta;                   // dense [B][Hv][L]
 };
 
 // ---------------------------------------------------------------- prep
@@ -44,9 +51,9 @@ __device__ __forceinline__ floatx4 mfma_f32(float a, float b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <typename T, int DK>
+template <typename T, int DK, int PO>
 __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu(3))) void k_gdr_prep(Args a, int64_t slots) {
-    constexpr int P = sizeof(T) == 2 ? 1 : 3, PO = sizeof(T) == 2 ? 2 : 3, KS = DK / 32;
+    constexpr int P = sizeof(T) == 2 ? 1 : 3, KS = DK / 32;
     struct Lds {
         __align__(16) float D[2][16][20];     // diagonal blocks of N diag(beta), by column
         __align__(16) float L10[16][20];
@@ -230,15 +237,20 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
 //             transition (columns of the identity, v = 0)
 //   kSave     for the gradients: E of every chunk and the state entering every
 //             save-th one
-enum Mode { kOut, kSegment, kSave };
+enum Mode { kOut, kSegment, kSave, kBack, kBackSegment };
+
+// Parts of TA in the records: two where its product is only rounded to bf16.
+template <typename T>
+constexpr int rec_parts(bool grads) { return sizeof(T) == 2 && !grads ? 2 : 3; }
 
 template <typename T, int DK, int MODE>
 struct Chunk {
     static constexpr int P = sizeof(T) == 2 ? 1 : 3;      // parts of q and k
     static constexpr int PO = sizeof(T) == 2 ? 2 : 3;     // parts of f32 operands of the output alone
-    static constexpr int NI = MODE == kOut ? 3 + PO : MODE == kSave ? 6 : 3;   // images: TW, then TA or T^
+    static constexpr bool HAS_Q = MODE != kSegment && MODE != kSave;
+    static constexpr int NI = MODE == kOut ? 3 + PO : MODE == kSegment ? 3 : 6;   // images: TW, then TA (kSave: T^)
     __align__(16) char K[P][32 * DK * 2];
-    __align__(16) char Q[MODE == kOut ? P : 1][MODE == kOut ? 32 * DK * 2 : 16];
+    __align__(16) char Q[HAS_Q ? P : 1][HAS_Q ? 32 * DK * 2 : 16];
     __align__(16) char M[NI][kImg];
     __align__(16) float eG[32];
 };
@@ -327,7 +339,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const uint32_t vo = live_col && value ? 4 * qd * vst + col * (uint32_t)sizeof(T) : kNone;
     const uint32_t oo = live_col ? 4 * qd * ost + col * (uint32_t)sizeof(T) : kNone;
     const uint32_t kst = (uint32_t)a.k.st * sizeof(T), qst = (uint32_t)a.q.st * sizeof(T);
-    const uint32_t rb = rec_bytes(PO, MODE == kSave);
+    const int rp = rec_parts<T>(a.grads);          // (of the record; this kernel stages what it needs)
+    const uint32_t rb = rec_bytes(rp, a.grads);
     uint32_t ko[KU], qo[KU];
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
@@ -353,9 +366,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
         for (int i = 0; i < MU; ++i) {
             const int u = tid + 256 * i < NI * 128 ? tid + 256 * i : tid;
-            rm[i] = *(const uintx4 *)(rec + (MODE == kSave && u >= 384 ? rec_rows(PO) + 256 - 384 * 16 : 0u) + 16u * u);
+            rm[i] = *(const uintx4 *)(rec + (MODE == kSave && u >= 384 ? rec_rows(rp) + 256 - 384 * 16 : 0u) + 16u * u);
         }
-        reG = *(const float *)(rec + rec_rows(PO) + 4 * (tid % 32));
+        reG = *(const float *)(rec + rec_rows(rp) + 4 * (tid % 32));
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -527,9 +540,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         lds_barrier();
     }
     if (!mine) return;
-    if constexpr (MODE == kSegment)
-        store_state(value ? a.segE + (slot * a.Hv + h) * a.dk * a.dv : a.tr + (slot * a.Hv + h) * DK * DK, value ? a.dv : DK);
-    else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv, a.dv);
+    if constexpr (MODE == kSegment) {
+        if (value) store_state(a.segE + (slot * a.Hv + h) * a.dk * a.dv, a.dv);
+        else if (live_col) {                       // by column: tr[col][key]
+            float *out = a.tr + (slot * a.Hv + h) * DK * DK + col * DK;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+                if (key0(kt) < a.dk) *(floatx4 *)(out + key0(kt)) = S[kt];
+        }
+    } else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv, a.dv);
 }
 
 }  // namespace gdr

@@ -1,0 +1,719 @@
+// libpgf: gradients of the gated delta rule for gfx950.
+//
+// In the chunk form of pgf_gdr.hip, with E the errors (the steps write
+// diag(beta) E), S0 and S1 the state entering and leaving a run of steps and
+// dO, dS1 the adjoints of its outputs and of S1:
+//   dE  = TW^T (K dS1) + scale TA^T dO                (dE is also dl/dV)
+//   dS0 = e^{G_C} dS1 + Q^T (scale e^G dO) - K^T (e^G dE)
+// so the adjoint runs through the chunks backwards with the forward chain's
+// products transposed, and needs neither S nor E.  Everything else follows, for
+// any run of steps (here 64), from E, dE, S0 and dS1.  With z_t = dS1 E_t,
+// y_t = S0 dE_t, decays c_st = e^{G_s - G_t}, and sums over steps of the run:
+//   dq_s = scale e^{G_s} S0 dO_s + sum_{t<=s} scale c_st beta_t (dO_s.E_t) k_t
+//   w_t  = e^{G_C - G_t} z_t + sum_{s>=t} scale c_st (dO_s.E_t) q_s - sum_{s>t} c_st (dE_s.E_t) k_s
+//   r_t  = -e^{G_t} y_t - sum_{u<t} c_tu beta_u (dE_t.E_u) k_u
+//   dk_t = beta_t w_t + r_t,   dbeta_t = k_t.w_t
+//   dG_t = q_t.dq_t + k_t.r_t - beta_t dbeta_t,  at the run's end also <dS1, S1>,
+//   dg   = sums of dG from each step to the run's end
+// (G_t enters wherever q_t reads the state or k_t reads it, against where k_t
+// writes it).  <dS1, S1> = e^{G_C} <dS1, S0> + sum_t e^{G_C - G_t} beta_t k_t.z_t.
+//
+//   k_gdr_prep                records, with T^
+//   k_gdr_chain<kSave>        forward: E, and S every 64 steps
+//   k_gdr_back                backwards: dE, dl/dv, and dS every 64 steps
+//   k_gdr_outer               per 64 steps and key head: dq, dk, dbeta, dg; the
+//                             value heads of a key head one after the other, so
+//                             their sums have an order
+#include "pgf_gdr_chain.h"
+#include "pgf_timing.h"
+
+namespace pgf {
+namespace gdr {
+
+// ---------------------------------------------------------------- backwards
+// As k_gdr_chain: a wave owns 16 value columns of the adjoint state of one head.
+// kBackSegment: from zero at the segment's end to its start, nothing written on
+// the way.
+template <typename T, int DK, int MODE>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_back(Args a, uint32_t n_items) {
+    using Ck = Chunk<T, DK, MODE>;
+    constexpr int P = Ck::P, NI = 6;
+    constexpr int KS = DK / 32, KT = DK / 16;
+    constexpr int KU = 32 * DK / 8 / 256, MU = NI * 128 / 256;
+    constexpr int NB = sizeof(Ck) <= 40960 ? 2 : 1;
+    __shared__ Ck lds[NB];
+    const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int cb = (a.vt + 3) / 4;
+    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const int64_t sh = item / cb;
+    const int tile = (int)(item - sh * cb) * 4 + w;
+    const int64_t slot = sh / a.Hv;
+    const int h = (int)(sh - slot * a.Hv), hk = h / a.rep;
+    const Rows r = a.seqs.of(slot, a.seg ? a.seg : a.seqs.L + 1, a.seg_per);
+    if (r.unit0 > 0 && r.unit0 >= r.len) return;   // uniform over the block
+    int64_t n = uni(r.len - r.unit0);
+    if (a.seg && n > a.seg) n = a.seg;
+    const bool mine = tile < a.vt;
+    const int col = tile * 16 + c;
+    const bool live_col = mine && col < a.dv;
+    const int chunks = (int)((n + kC - 1) / kC);
+    const int64_t t0 = r.lo + r.unit0;
+    const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
+    const int64_t save0 = uni(a.seqs.slot0(r.n, kC * kSuper, a.save_per) + r.unit0 / (kC * kSuper));
+
+    auto key0 = [&](int kt) { return 32 * (kt / 2) + 8 * qd + 4 * (kt & 1); };
+    floatx4 S[KT];                                 // the adjoint
+    {
+        const float *in = MODE == kBackSegment ? nullptr : a.dseg_in ? a.dseg_in + (slot * a.Hv + h) * a.dk * a.dv
+                          : a.dS_out ? a.dS_out + (r.n * a.Hv + h) * a.dk * a.dv : nullptr;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (in) {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const bool on = live_col && key0(kt) < a.dk;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    S[kt][j] = *at_off(in, (uint32_t)(on ? (key0(kt) + j) * a.dv + col : 0) * 4u);
+            }
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+                if (!(live_col && key0(kt) < a.dk)) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+    }
+    auto store_state = [&](float *out) {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+            if (live_col && key0(kt) < a.dk) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *at_off(out, (uint32_t)((key0(kt) + j) * a.dv + col) * 4u) = S[kt][j];
+            }
+    };
+
+    Raw8<T> rk[KU], rq[KU];
+    uintx4 rm[MU];
+    float reG;
+    uint32_t ro[2][4];
+    const T *kp = row_ptr<T>(a.k, r.b, hk, t0), *qp = row_ptr<T>(a.q, r.b, hk, t0), *gp = row_ptr<T>(a.go, r.b, h, t0),
+            *vp = row_ptr<T>(a.dv_, r.b, h, t0);
+    const uint32_t gst = (uint32_t)a.go.st * sizeof(T), vst = (uint32_t)a.dv_.st * sizeof(T);
+    const uint32_t kst = (uint32_t)a.k.st * sizeof(T), qst = (uint32_t)a.q.st * sizeof(T);
+    const uint32_t go = live_col ? 4 * qd * gst + col * (uint32_t)sizeof(T) : kNone;
+    const uint32_t vo = live_col ? 4 * qd * vst + col * (uint32_t)sizeof(T) : kNone;
+    const uint32_t rb = rec_bytes(3, true);
+    uint32_t ko[KU], qo[KU];
+#pragma unroll
+    for (int i = 0; i < KU; ++i) {
+        const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
+        ko[i] = e < a.dk ? t * kst + e * (uint32_t)sizeof(T) : kNone;
+        qo[i] = e < a.dk ? t * qst + e * (uint32_t)sizeof(T) : kNone;
+    }
+    auto live_rows = [&](int ch) {
+        const int64_t left = n - (int64_t)ch * kC;
+        return (int)(left < kC ? left : kC);
+    };
+    auto fetch = [&](int ch) {
+        const int live = live_rows(ch);
+        const Buf kb = make_buf(kp + (int64_t)ch * kC * a.k.st, kst, live, a.dk * (int)sizeof(T));
+        const Buf qb = make_buf(qp + (int64_t)ch * kC * a.q.st, qst, live, a.dk * (int)sizeof(T));
+        const Buf gb = make_buf(gp + (int64_t)ch * kC * a.go.st, gst, live, a.dv * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            rk[i] = load8<T>(kb, ko[i], 0);
+            rq[i] = load8<T>(qb, qo[i], 0);
+        }
+        const char *rec = a.rec + ((slot0 + ch) * a.Hv + h) * (int64_t)rb;
+#pragma unroll
+        for (int i = 0; i < MU; ++i) rm[i] = *(const uintx4 *)(rec + 16u * (tid + 256 * i));
+        reG = *(const float *)(rec + rec_rows(3) + 4 * (tid % 32));
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ro[m][j] = load1<T>(gb, go, (16 * m + j) * gst);
+    };
+    auto stage = [&](Ck &s) {
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int u = tid + 256 * i, t = u / (DK / 8);
+            const uint32_t at = unit_off<DK>(t, u % (DK / 8));
+            const Frag<P> f = raw_frag<P>(rk[i]), y = raw_frag<P>(rq[i]);
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                *(bf16x8 *)&s.K[p][at] = f.p[p];
+                *(bf16x8 *)&s.Q[p][at] = y.p[p];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MU; ++i) *(uintx4 *)(&s.M[0][0] + 16 * (tid + 256 * i)) = rm[i];
+        if (tid < 32) s.eG[tid] = reG;
+    };
+
+    if (chunks > 0) {
+        fetch(chunks - 1);
+        stage(lds[0]);
+        lds_barrier();
+    }
+    for (int i = 0; i < chunks; ++i) {
+        const int ch = chunks - 1 - i;
+        if constexpr (MODE == kBack)
+            if (mine && (i == 0 || ch % kSuper == kSuper - 1))
+                store_state(a.saveD + ((save0 + ch / kSuper) * a.Hv + h) * a.dk * a.dv);
+        float g[2][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[m][j] = raw_f<T>(ro[m][j]);
+        const Ck &s = lds[NB == 2 ? i & 1 : 0];
+        fetch(ch > 0 ? ch - 1 : 0);                // (the first chunk again rather than a branch)
+        if (mine) {
+            floatx4 x[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) x[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+            Frag<P> kf[2][2];
+            auto read_k = [&](int ks) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        kf[ks & 1][m].p[p] = *(const bf16x8 *)&s.K[p][unit_off<DK>(16 * m + c, 4 * ks + qd)];
+            };
+            // rows 16 m + c of the transposed images (TW^T: 0, TA^T: 3)
+            auto read_mt = [&](int first, Frag<3> (&f)[2]) {
+                const int row = 4 * qd + c / 4;
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) {
+                        const char *m0 = &s.M[first + p][unit_off<32>(row, c % 4) + 8 * m];
+                        const char *m1 = &s.M[first + p][unit_off<32>(16 + row, c % 4) + 8 * m];
+                        f[m].p[p] = __builtin_shufflevector(read_tr(m0), read_tr(m1), 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
+            };
+            Frag<3> af[2], tf[2];
+            floatx4 eG[2], dE[2];
+            read_k(0);
+            read_mt(3, af);
+            const Frag<P> gf = to_frag<P>(floatx4{g[0][0], g[0][1], g[0][2], g[0][3]},
+                                          floatx4{g[1][0], g[1][1], g[1][2], g[1][3]});
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if (ks + 1 < KS) read_k(ks + 1);
+                else {
+                    read_mt(0, tf);
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) eG[m] = *(const floatx4 *)&s.eG[16 * m + 4 * qd];
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (ks == 0) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) dE[m] = mfma_parts<3, P>(af[m], gf, floatx4{0.0f, 0.0f, 0.0f, 0.0f});
+                }
+                const Frag<3> sp = to_frag<3>(S[2 * ks], S[2 * ks + 1]);
+#pragma unroll
+                for (int m = 0; m < 2; ++m) x[m] = mfma_parts<P, 3>(kf[ks & 1][m], sp, x[m]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const Frag<3> xp = to_frag<3>(x[0], x[1]);
+            constexpr int GK = P == 1 ? 4 : 1;
+            Frag<P> ktf[2][GK], qtf[2][GK];
+            auto read_kt = [&](int gr) {
+#pragma unroll
+                for (int e = 0; e < GK; ++e) {
+                    const int kt = gr * GK + e, row = 4 * qd + c / 4;
+                    const uint32_t o0 = unit_off<DK>(row, 4 * (kt / 2) + c % 4) + 8 * (kt & 1);
+                    const uint32_t o1 = unit_off<DK>(16 + row, 4 * (kt / 2) + c % 4) + 8 * (kt & 1);
+#pragma unroll
+                    for (int p = 0; p < P; ++p) {
+                        ktf[gr & 1][e].p[p] =
+                            __builtin_shufflevector(read_tr(&s.K[p][o0]), read_tr(&s.K[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
+                        qtf[gr & 1][e].p[p] =
+                            __builtin_shufflevector(read_tr(&s.Q[p][o0]), read_tr(&s.Q[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
+                    }
+                }
+            };
+            read_kt(0);
+            const float end = s.eG[31];
+            __builtin_amdgcn_sched_barrier(0);
+            floatx4 gs[2], es[2];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    dE[m][j] *= a.scale;
+                    gs[m][j] = a.scale * eG[m][j] * g[m][j];
+                }
+                dE[m] = mfma_parts<3, 3>(tf[m], xp, dE[m]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) es[m][j] = -eG[m][j] * dE[m][j];
+            }
+            const Frag<3> gp3 = to_frag<3>(gs[0], gs[1]), ep3 = to_frag<3>(es[0], es[1]);
+#pragma unroll
+            for (int gr = 0; gr < KT / GK; ++gr) {
+                if (gr + 1 < KT / GK) read_kt(gr + 1);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int e = 0; e < GK; ++e)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) S[gr * GK + e][j] *= end;
+#pragma unroll
+                for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        if (sum - p >= 0) {
+#pragma unroll
+                            for (int e = 0; e < GK; ++e)
+                                S[gr * GK + e] = mfma(qtf[gr & 1][e].p[p], gp3.p[sum - p], S[gr * GK + e]);
+#pragma unroll
+                            for (int e = 0; e < GK; ++e)
+                                S[gr * GK + e] = mfma(ktf[gr & 1][e].p[p], ep3.p[sum - p], S[gr * GK + e]);
+                        }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr (MODE == kBack) {
+                float *eb = a.saveU + ((slot0 + ch) * a.Hv + h) * (int64_t)(kC * a.dv);
+                const Buf vb = make_buf(vp + (int64_t)ch * kC * a.dv_.st, vst, live_rows(ch), a.dv * (int)sizeof(T));
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) store1<T>(vb, vo, (16 * m + j) * vst, dE[m][j]);
+                if (live_col) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            *at_off(eb, (uint32_t)((16 * m + 4 * qd + j) * a.dv + col) * 4u) = dE[m][j];
+                }
+            }
+        }
+        if constexpr (NB == 1) lds_barrier();
+        stage(lds[NB == 2 ? (i + 1) & 1 : 0]);
+        lds_barrier();
+    }
+    if (!mine) return;
+    if constexpr (MODE == kBackSegment) store_state(a.dsegE + (slot * a.Hv + h) * a.dk * a.dv);
+    else if (a.dS_in && r.unit0 == 0) store_state(a.dS_in + (r.n * a.Hv + h) * a.dk * a.dv);
+}
+
+// ---------------------------------------------------------------- outer
+// A block takes 64 steps of one key head; wave w their tile of 16 steps 16 w ..
+// as columns of every product, and all keys as rows, so that the sums over
+// keys (dbeta, dG) stay in a wave.  Phase one runs over the value columns, 32
+// at a time through LDS in three parts: z = dS1 E, y = S0 dE, S0 dO, and the
+// 64 x 64 products of E, dE and dO, each in the orientation its next product
+// wants it as operand.  Phase two adds the products with K and Q.
+// Bound by the matrix cores (2850 instructions a block and head at 128 x 128)
+// and by the reads of S0 and dS1.
+constexpr int kRun = kC * kSuper;
+
+template <typename T, int DK>
+struct OuterLds {
+    static constexpr int P = sizeof(T) == 2 ? 1 : 3;
+    union {
+        struct {
+            __align__(16) char S0[3][DK * 64], S1[3][DK * 64];       // rows of 32 value columns
+            __align__(16) char E[3][kRun * 64], dE[3][kRun * 64], dO[P][kRun * 64];
+        } v;
+        struct {
+            __align__(16) char K[P][kRun * DK * 2], Q[P][kRun * DK * 2];
+        } k;
+    };
+    double G[kRun];
+    float be[kRun], dG[kRun], kz[kRun], dot[4];
+};
+
+template <typename T, int DK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1))) void k_gdr_outer(Args a, uint32_t n_items) {
+    constexpr int P = sizeof(T) == 2 ? 1 : 3;
+    constexpr int KT = DK / 16, SU = DK / 64, KU = kRun * DK / 8 / 256;
+    __shared__ OuterLds<T, DK> lds;
+    const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const int64_t sslot = item / a.Hk;
+    const int hk = (int)(item - sslot * a.Hk);
+    const Rows r = a.seqs.of(sslot, kRun, a.save_per);
+    if (r.unit0 >= r.len) return;                  // uniform over the block
+    const int live = (int)uni(r.len - r.unit0 < kRun ? r.len - r.unit0 : kRun);
+    const int64_t t0 = uni(r.lo + r.unit0);
+    const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
+    const int tok = 16 * w + c;                    // this lane's step
+
+    floatx4 dqs[KT], dks[KT];                      // sums over the value heads
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) dqs[kt] = dks[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int vh = 0; vh < a.rep; ++vh) {
+        const int h = hk * a.rep + vh;
+        lds_barrier();                             // (the last head's reads)
+        if (w == 0) {
+            float g = 0.0f, be = 0.0f;
+            if (lane < live) {
+                g = *a.g.at<const float>(r.b, h, t0 + lane);
+                be = *a.beta.at<const float>(r.b, h, t0 + lane);
+                g = g < -200.0f ? -200.0f : g;
+            }
+            double G = g;
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) {
+                const double o = __shfl_up(G, m, 64);
+                if (lane >= m) G += o;
+            }
+            lds.G[lane] = G;
+            lds.be[lane] = be;
+        }
+        // ---- phase one
+        floatx4 z[KT], y[KT], o[KT], d1t[4], d1s[4], d2t[4], d2s[4];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) z[kt] = y[kt] = o[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d1t[i] = d1s[i] = d2t[i] = d2s[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        float ss = 0.0f;                           // <dS1, S0>
+        const int64_t cell = (sslot * a.Hv + h) * (int64_t)(a.dk * a.dv);
+        const Buf s0b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveS + cell)), a.dv * 4, a.dk, a.dv * 4);
+        const Buf s1b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveD + cell)), a.dv * 4, a.dk, a.dv * 4);
+        const Buf gb = make_buf(row_ptr<T>(a.go, r.b, h, t0), (uint32_t)a.go.st * sizeof(T), live, a.dv * (int)sizeof(T));
+        const int er = tid / 4, eu = tid % 4;      // row and unit of E, dE and dO
+        const bool elive = er < live;
+        const int64_t eat = ((slot0 + (elive ? er / kC : 0)) * a.Hv + h) * (int64_t)(kC * a.dv) + (elive ? er % kC * a.dv : 0);
+        Raw8<float> r0[SU], r1[SU], re, rd;
+        Raw8<T> rg;
+        bool con;                                  // this thread's columns are there
+        auto fetch = [&](int v0) {
+            con = v0 + 8 * eu < a.dv;
+            const uint32_t vc = (uint32_t)(v0 + 8 * eu);
+#pragma unroll
+            for (int i = 0; i < SU; ++i) {
+                const uint32_t at = con ? (uint32_t)(er + 64 * i) * (a.dv * 4u) + vc * 4u : kNone;
+                r0[i] = load8<float>(s0b, at, 0);
+                r1[i] = load8<float>(s1b, at, 0);
+            }
+            const float *ep = a.saveE + eat + (con ? vc : 0), *dp = a.saveU + eat + (con ? vc : 0);
+            re.x = *(const uintx4 *)ep;
+            re.y = *(const uintx4 *)(ep + 4);
+            rd.x = *(const uintx4 *)dp;
+            rd.y = *(const uintx4 *)(dp + 4);
+            rg = load8<T>(gb, con ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
+        };
+        fetch(0);
+        for (int v0 = 0; v0 < a.dv; v0 += 32) {
+            if (v0) lds_barrier();                 // the last columns' reads
+            {
+                const uint32_t at = unit_off<32>(er, eu);
+                if (!(con && elive)) {
+                    re.x = re.y = uintx4{};
+                    rd.x = rd.y = uintx4{};
+                }
+                const Frag<3> fe = raw_frag<3>(re), fd = raw_frag<3>(rd);
+                const Frag<P> fg = raw_frag<P>(rg);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    *(bf16x8 *)&lds.v.E[p][at] = fe.p[p];
+                    *(bf16x8 *)&lds.v.dE[p][at] = fd.p[p];
+                }
+#pragma unroll
+                for (int p = 0; p < P; ++p) *(bf16x8 *)&lds.v.dO[p][at] = fg.p[p];
+#pragma unroll
+                for (int i = 0; i < SU; ++i) {
+                    const uint32_t sa = unit_off<32>(er + 64 * i, eu);
+                    const Frag<3> f0 = raw_frag<3>(r0[i]), f1 = raw_frag<3>(r1[i]);
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) {
+                        *(bf16x8 *)&lds.v.S0[p][sa] = f0.p[p];
+                        *(bf16x8 *)&lds.v.S1[p][sa] = f1.p[p];
+                    }
+                    const floatx4 x0 = __builtin_bit_cast(floatx4, r0[i].x), x1 = __builtin_bit_cast(floatx4, r1[i].x);
+                    const floatx4 y0 = __builtin_bit_cast(floatx4, r0[i].y), y1 = __builtin_bit_cast(floatx4, r1[i].y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ss = fmaf(x0[j], x1[j], fmaf(y0[j], y1[j], ss));
+                }
+            }
+            fetch(v0 + 32 < a.dv ? v0 + 32 : v0);
+            lds_barrier();
+            Frag<3> ew, dw;                        // this wave's steps as columns
+            Frag<P> gw;
+            const uint32_t wa = unit_off<32>(16 * w + c, qd);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                ew.p[p] = *(const bf16x8 *)&lds.v.E[p][wa];
+                dw.p[p] = *(const bf16x8 *)&lds.v.dE[p][wa];
+            }
+#pragma unroll
+            for (int p = 0; p < P; ++p) gw.p[p] = *(const bf16x8 *)&lds.v.dO[p][wa];
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                Frag<3> f0, f1;
+                const uint32_t at = unit_off<32>(16 * kt + c, qd);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    f0.p[p] = *(const bf16x8 *)&lds.v.S0[p][at];
+                    f1.p[p] = *(const bf16x8 *)&lds.v.S1[p][at];
+                }
+                z[kt] = mfma_parts<3, 3>(f1, ew, z[kt]);
+                y[kt] = mfma_parts<3, 3>(f0, dw, y[kt]);
+                o[kt] = mfma_parts<3, P>(f0, gw, o[kt]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                Frag<3> fe, fd;
+                Frag<P> fg;
+                const uint32_t at = unit_off<32>(16 * i + c, qd);
+                if (i <= w) {                      // (uniform over the wave)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) fe.p[p] = *(const bf16x8 *)&lds.v.E[p][at];
+                    d1t[i] = mfma_parts<3, P>(fe, gw, d1t[i]);
+                    d2t[i] = mfma_parts<3, 3>(fe, dw, d2t[i]);
+                }
+                if (i >= w) {
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) fd.p[p] = *(const bf16x8 *)&lds.v.dE[p][at];
+#pragma unroll
+                    for (int p = 0; p < P; ++p) fg.p[p] = *(const bf16x8 *)&lds.v.dO[p][at];
+                    d1s[i] = mfma_parts<P, 3>(fg, ew, d1s[i]);
+                    d2s[i] = mfma_parts<3, 3>(fd, ew, d2s[i]);
+                }
+            }
+        }
+        // ---- phase two
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) ss += __shfl_xor(ss, m, 64);
+        if (lane == 0) lds.dot[w] = ss;
+        lds_barrier();                             // phase one's reads
+        {
+            const Buf kb = make_buf(row_ptr<T>(a.k, r.b, hk, t0), (uint32_t)a.k.st * sizeof(T), live, a.dk * (int)sizeof(T));
+            const Buf qb = make_buf(row_ptr<T>(a.q, r.b, hk, t0), (uint32_t)a.q.st * sizeof(T), live, a.dk * (int)sizeof(T));
+            Raw8<T> rk[KU], rq[KU];
+#pragma unroll
+            for (int i = 0; i < KU; ++i) {
+                const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
+                rk[i] = load8<T>(kb, e < a.dk ? t * kb.st + e * (uint32_t)sizeof(T) : kNone, 0);
+                rq[i] = load8<T>(qb, e < a.dk ? t * qb.st + e * (uint32_t)sizeof(T) : kNone, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < KU; ++i) {
+                const int u = tid + 256 * i, t = u / (DK / 8);
+                const uint32_t at = unit_off<DK>(t, u % (DK / 8));
+                const Frag<P> f = raw_frag<P>(rk[i]), x = raw_frag<P>(rq[i]);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    *(bf16x8 *)&lds.k.K[p][at] = f.p[p];
+                    *(bf16x8 *)&lds.k.Q[p][at] = x.p[p];
+                }
+            }
+        }
+        const double Gt = lds.G[tok], Gend = lds.G[kRun - 1];
+        const float eG = expf((float)Gt), out = expf((float)(Gend - Gt)), be = lds.be[tok];
+        // decays and signs of the 64 x 64 products; what has no place is zero
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int row = 16 * i + 4 * qd + j;
+                const float dG = (float)(Gt - lds.G[row]);
+                const float e = expf(row <= tok ? dG : -dG);         // both directions decay
+                const float br = lds.be[row];
+                d1t[i][j] = row <= tok ? a.scale * e * br * d1t[i][j] : 0.0f;
+                d2t[i][j] = row < tok ? -e * br * d2t[i][j] : 0.0f;
+                d1s[i][j] = row >= tok ? a.scale * e * d1s[i][j] : 0.0f;
+                d2s[i][j] = row > tok ? -e * d2s[i][j] : 0.0f;
+            }
+        lds_barrier();
+        // keys 16 kt + 4 qd .. of this lane's step
+        auto row4 = [&](const char (*m)[kRun * DK * 2], int kt) {
+            floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int p = P - 1; p >= 0; --p)
+                x += __builtin_convertvector(*(const bf16x4 *)&m[p][unit_off<DK>(tok, 2 * kt + qd / 2) + 8 * (qd & 1)], floatx4);
+            return x;
+        };
+        float kz = 0.0f, qdq = 0.0f, kr = 0.0f, kw = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const floatx4 kx = row4(lds.k.K, kt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                z[kt][j] *= out;
+                y[kt][j] *= -eG;
+                o[kt][j] *= a.scale * eG;
+                kz = fmaf(kx[j], z[kt][j], kz);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const bool early = 2 * b <= w, late = 2 * b + 1 >= w;    // (uniform over the wave)
+            const Frag<3> f1t = to_frag<3>(d1t[2 * b], d1t[2 * b + 1]), f2t = to_frag<3>(d2t[2 * b], d2t[2 * b + 1]);
+            const Frag<3> f1s = to_frag<3>(d1s[2 * b], d1s[2 * b + 1]), f2s = to_frag<3>(d2s[2 * b], d2s[2 * b + 1]);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                Frag<P> kf, qf;
+                const int row = 32 * b + 4 * qd + c / 4, p4 = c % 4;
+                const uint32_t o0 = unit_off<DK>(row, 2 * kt + p4 / 2) + 8 * (p4 & 1);
+                const uint32_t o1 = unit_off<DK>(row + 16, 2 * kt + p4 / 2) + 8 * (p4 & 1);
+#pragma unroll
+                for (int p = 0; p < P; ++p) {
+                    kf.p[p] = __builtin_shufflevector(read_tr(&lds.k.K[p][o0]), read_tr(&lds.k.K[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
+                    qf.p[p] = __builtin_shufflevector(read_tr(&lds.k.Q[p][o0]), read_tr(&lds.k.Q[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+                if (early) {
+                    o[kt] = mfma_parts<P, 3>(kf, f1t, o[kt]);
+                    y[kt] = mfma_parts<P, 3>(kf, f2t, y[kt]);
+                }
+                if (late) {
+                    z[kt] = mfma_parts<P, 3>(qf, f1s, z[kt]);
+                    z[kt] = mfma_parts<P, 3>(kf, f2s, z[kt]);
+                }
+            }
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const floatx4 kx = row4(lds.k.K, kt), qx = row4(lds.k.Q, kt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                kw = fmaf(kx[j], z[kt][j], kw);
+                kr = fmaf(kx[j], y[kt][j], kr);
+                qdq = fmaf(qx[j], o[kt][j], qdq);
+                dqs[kt][j] += o[kt][j];
+                dks[kt][j] += fmaf(be, z[kt][j], y[kt][j]);
+            }
+        }
+#pragma unroll
+        for (int m = 16; m < 64; m *= 2) {
+            kz += __shfl_xor(kz, m, 64);
+            kw += __shfl_xor(kw, m, 64);
+            kr += __shfl_xor(kr, m, 64);
+            qdq += __shfl_xor(qdq, m, 64);
+        }
+        if (qd == 0) {
+            lds.dG[tok] = qdq + kr - be * kw;
+            lds.kz[tok] = be * kz;
+            if (tok < live) a.dbeta[(r.b * a.Hv + h) * a.seqs.L + t0 + tok] = kw;
+        }
+        lds_barrier();
+        if (w == 0) {
+            double v = lds.dG[lane], e = lds.kz[lane];
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) e += __shfl_xor(e, m, 64);
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) {
+                const double x = __shfl_down(v, m, 64);
+                if (lane + m < 64) v += x;
+            }
+            const double s01 = (double)lds.dot[0] + lds.dot[1] + lds.dot[2] + lds.dot[3];
+            if (lane < live)
+                a.dg[(r.b * a.Hv + h) * a.seqs.L + t0 + lane] = (float)(v + e + (double)expf((float)Gend) * s01);
+        }
+    }
+    if (tok >= live) return;
+    T *dq = a.dq.at<T>(r.b, hk, t0 + tok), *dk = a.dk_.at<T>(r.b, hk, t0 + tok);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+        const int key = 16 * kt + 4 * qd;
+        if (key < a.dk) {
+            Raw4<T> x, u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x.x[j] = (T)dqs[kt][j];
+                u.x[j] = (T)dks[kt][j];
+            }
+            *(Raw4<T> *)(dq + key) = x;
+            *(Raw4<T> *)(dk + key) = u;
+        }
+    }
+}
+
+// ---------------------------------------------------------------- dispatch
+View view(const void *p, const int64_t (&s)[3], int64_t H, int64_t L, int64_t d);
+Args make_args(const Plan &pl, const pgf_gdr_params *p, const void *q, const void *k, const void *v, const float *g,
+               const float *beta, const void *o);
+int check_arrays(const Plan &pl, const pgf_gdr_params *p, const void *q, const void *k, const void *v, const float *g,
+                 const float *beta, const void *o);
+
+template <typename T, int DK>
+int grads_t(Args a, const Plan &pl, hipStream_t st) {
+    const int64_t items = pl.chunk_slots * pl.Hk;
+    if (items) {
+        Timed tm(0, st);
+        hipLaunchKernelGGL((k_gdr_prep<T, DK, 3>), dim3((unsigned)((items + kPrepWaves - 1) / kPrepWaves)),
+                           dim3(64 * kPrepWaves), 0, st, a, pl.chunk_slots);
+    }
+    const uint32_t blocks = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
+    if (items) {
+        Timed tm(1, st);
+        hipLaunchKernelGGL((k_gdr_chain<T, DK, kSave>), dim3(blocks), dim3(256), 0, st, a, blocks);
+    }
+    {
+        Timed tm(2, st);
+        hipLaunchKernelGGL((k_gdr_back<T, DK, kBack>), dim3(blocks), dim3(256), 0, st, a, blocks);
+    }
+    if (items) {
+        Timed tm(3, st);
+        const uint32_t n = (uint32_t)(pl.super_slots * pl.Hk);
+        hipLaunchKernelGGL((k_gdr_outer<T, DK>), dim3(n), dim3(256), 0, st, a, n);
+    }
+    return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;
+}
+
+}  // namespace gdr
+}  // namespace pgf
+
+extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const float *g, const float *beta,
+                             const void *do_, const pgf_gdr_params *p, void *dq, void *dk, void *dv, float *dg,
+                             float *dbeta, void *stream) {
+    using namespace pgf;
+    using namespace pgf::gdr;
+    Plan pl;
+    int rc = make_plan(p, &pl, true, false);
+    if (rc != PGF_OK) return rc;
+    rc = check_arrays(pl, p, q, k, v, g, beta, do_);
+    if (rc != PGF_OK) return rc;
+    if (pl.L > 0 && (!dq || !dk || !dv || !dg || !dbeta)) return PGF_ERR_INVALID_ARG;
+    if (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 15) return PGF_ERR_INVALID_ARG;
+    if (!p->workspace || p->workspace_bytes < pl.total || ((uintptr_t)p->workspace & 255)) return PGF_ERR_WORKSPACE;
+    const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;
+    const size_t ns = (size_t)(pl.nseq * pl.Hv * pl.dk * pl.dv) * 4, ng = (size_t)(pl.B * pl.Hv * pl.L) * 4;
+    const struct { const void *p; size_t n; } ins[] = {
+        {q, extent(p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e)}, {k, extent(p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e)},
+        {v, extent(p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {g, extent(p->g_strides, pl.B, pl.Hv, pl.L, 1, 4)},
+        {beta, extent(p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4)},
+        {do_, extent(p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {p->S_in, ns}, {p->dS_out, ns}};
+    const struct { const void *p; size_t n; } outs[] = {
+        {dq, extent(p->dq_strides, pl.B, pl.Hk, pl.L, pl.dk, e)}, {dk, extent(p->dk_strides, pl.B, pl.Hk, pl.L, pl.dk, e)},
+        {dv, extent(p->dv_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {dg, ng}, {dbeta, ng}, {p->dS_in, ns}};
+    for (const auto &o : outs) {
+        for (const auto &i : ins)
+            if (overlaps(o.p, o.n, i.p, i.n)) return PGF_ERR_INVALID_ARG;
+        if (overlaps(p->workspace, pl.total, o.p, o.n)) return PGF_ERR_INVALID_ARG;
+    }
+    for (const auto &i : ins)
+        if (overlaps(p->workspace, pl.total, i.p, i.n)) return PGF_ERR_INVALID_ARG;
+    // (dq, dk and dv may be parts of one array's rows: only the dense outputs are checked against each other)
+    for (int i = 3; i < 6; ++i)
+        for (int j = 0; j < i; ++j)
+            if (overlaps(outs[i].p, outs[i].n, outs[j].p, outs[j].n)) return PGF_ERR_INVALID_ARG;
+    (void)hipGetLastError();
+    Args a = make_args(pl, p, q, k, v, g, beta, nullptr);
+    a.go = view(do_, p->o_strides, pl.Hv, pl.L, pl.dv);
+    a.dq = view(dq, p->dq_strides, pl.Hk, pl.L, pl.dk);
+    a.dk_ = view(dk, p->dk_strides, pl.Hk, pl.L, pl.dk);
+    a.dv_ = view(dv, p->dv_strides, pl.Hv, pl.L, pl.dv);
+    char *ws = (char *)p->workspace;
+    a.rec = ws + pl.rec;
+    a.grads = 1;
+    a.segE = (float *)(ws + pl.segE);
+    a.tr = (float *)(ws + pl.tr);
+    a.S_in = p->S_in;
+    a.dS_out = p->dS_out;
+    a.dS_in = p->dS_in;
+    a.saveS = (float *)(ws + pl.S);
+    a.saveD = (float *)(ws + pl.dS);
+    a.saveE = (float *)(ws + pl.u);
+    a.saveU = (float *)(ws + pl.du);
+    a.dsegE = (float *)(ws + pl.dseg);
+    a.save = kSuper;
+    a.save_per = pl.supers_per;
+    a.dg = dg;
+    a.dbeta = dbeta;
+    hipStream_t st = (hipStream_t)stream;
+    const bool bf = p->in_dtype == PGF_BF16;
+    if (pl.DK == 64) return bf ? grads_t<__bf16, 64>(a, pl, st) : grads_t<float, 64>(a, pl, st);
+    return bf ? grads_t<__bf16, 128>(a, pl, st) : grads_t<float, 128>(a, pl, st);
+}

@@ -71,7 +71,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     if (q.dk % 8 || q.dk > 128 || q.dv % 8 || q.dv > 4096) return PGF_ERR_UNSUPPORTED;
     if (q.B > kMaxBatch || q.Hv > kMaxHeads || q.L > kMaxLen || p->n_seqs > kMaxBatch) return PGF_ERR_UNSUPPORTED;
     if (p->n_seqs && (q.B != 1 || step)) return PGF_ERR_INVALID_ARG;
-    if (p->seg_len < -1 || (p->seg_len > 0 && p->seg_len % kC)) return PGF_ERR_INVALID_ARG;
+    if (p->seg_len < -1 || (p->seg_len > 0 && p->seg_len % (kSuper * kC))) return PGF_ERR_INVALID_ARG;
     const int64_t unit = p->in_dtype == PGF_BF16 ? 8 : 4;
     const struct { const int64_t (&s)[3]; int64_t unit; bool out; int64_t heads; } arrays[] = {
         {p->q_strides, unit, false, q.Hk}, {p->k_strides, unit, false, q.Hk}, {p->v_strides, unit, false, q.Hv},
@@ -100,11 +100,13 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
     q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
     const int64_t cell = q.Hv * q.dk * q.dv * 4, cell_tr = q.Hv * (int64_t)q.DK * q.DK * 4;
-    q.rec_bytes = kImgBytes * (p->in_dtype == PGF_BF16 ? 5 : 6) + 256 + (grads ? 3 * kImgBytes : 0);
-    const int64_t ns = q.seg ? q.seg_slots : 0, nc = grads ? q.chunk_slots : 0;
+    q.rec_bytes = kImgBytes * (p->in_dtype == PGF_BF16 && !grads ? 5 : 6) + 256 + (grads ? 3 * kImgBytes : 0);
+    q.supers_per = cdiv(q.L, kSuper * kC);
+    q.super_slots = p->n_seqs ? q.L / (kSuper * kC) + p->n_seqs : q.B * q.supers_per;
+    const int64_t ns = q.seg ? q.seg_slots : 0, nc = grads ? q.chunk_slots : 0, nu = grads ? q.super_slots : 0;
     bool ok = section(&q.total, &q.rec, q.chunk_slots, q.Hv * q.rec_bytes);
     ok = ok && section(&q.total, &q.segE, ns, cell) && section(&q.total, &q.tr, ns, cell_tr);
-    ok = ok && section(&q.total, &q.S, nc, cell) && section(&q.total, &q.dS, nc, cell);
+    ok = ok && section(&q.total, &q.S, nu, cell) && section(&q.total, &q.dS, nu, cell);
     ok = ok && section(&q.total, &q.u, nc, q.Hv * kC * q.dv * 4) && section(&q.total, &q.du, nc, q.Hv * kC * q.dv * 4);
     ok = ok && section(&q.total, &q.dseg, grads ? ns : 0, cell);
     if (!ok) return PGF_ERR_UNSUPPORTED;

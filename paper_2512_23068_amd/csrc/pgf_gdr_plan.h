@@ -12,6 +12,7 @@ namespace pgf {
 namespace gdr {
 
 constexpr int kC = 32;           // steps per chunk
+constexpr int kSuper = 2;        // chunks between saved states of the gradients
 constexpr int64_t kImgBytes = 2048;  // a 32 x 32 matrix of bf16
 
 // Workspace sections (bytes, 256-byte aligned).
@@ -20,9 +21,9 @@ constexpr int64_t kImgBytes = 2048;  // a 32 x 32 matrix of bf16
 //                                             then (in place) its entry state
 //   tr    [segment slots][Hv][DK][DK]         transition of a segment
 // gradients:
-//   S     [chunk slots][Hv][dk][dv]           state entering each chunk
-//   dS    [chunk slots][Hv][dk][dv]           its adjoint leaving each chunk
-//   u, du [chunk slots][Hv][32][dv]           V' and dR of each chunk
+//   S     [super slots][Hv][dk][dv]           state entering every kSuper chunks
+//   dS    [super slots][Hv][dk][dv]           its adjoint leaving them
+//   u, du [chunk slots][Hv][32][dv]           E and its adjoint of each chunk
 //   dseg  [segment slots][Hv][dk][dv]         as seg, of the adjoint
 struct Plan {
     int64_t B, Hk, Hv, L, dk, dv, nseq;
@@ -30,6 +31,7 @@ struct Plan {
     int64_t chunk_slots, chunks_per;     // slots of kC steps, of a dense sequence
     int64_t seg;                 // steps per segment, 0 = sequences are not cut
     int64_t seg_slots, segs_per;
+    int64_t super_slots, supers_per;     // slots of kSuper * kC steps
     int64_t rec_bytes;           // of one chunk's record
     size_t rec, segE, tr, S, dS, u, du, dseg, total;
 };
