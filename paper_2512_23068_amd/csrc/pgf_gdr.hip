@@ -201,6 +201,18 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
     }
     a.S_in = p->S_in;
     a.S_out = p->S_out;
+    if (pl.seg) {
+        {
+            Args s = a;
+            s.ct = a.vt + (int)((pl.dk + 15) / 16);
+            const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
+            Timed tm(1, st);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(items), dim3(256), 0, st, s, items);
+        }
+        Timed tm(2, st);
+        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt)), dim3(256), 0, st, a);
+        a.seg_in = a.segE;
+    }
     const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
     Timed tm(3, st);
     hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut>), dim3(items), dim3(256), 0, st, a, items);
@@ -251,7 +263,7 @@ extern "C" int pgf_gdr_scan(const void *q, const void *k, const void *v, const f
         {beta, extent(p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4)}, {p->S_in, ns}};
     for (const auto &i : ins)
         if (overlaps(o, no, i.p, i.n) || overlaps(p->workspace, pl.total, i.p, i.n)) return PGF_ERR_INVALID_ARG;
-    // S_out may be S_in (each state is read before it is written) unless segments read it again.
+    // S_out may be S_in: a state is read before its sequence's last step writes it.
     for (int i = 0; i < 5; ++i)
         if (overlaps(p->S_out, ns, ins[i].p, ins[i].n)) return PGF_ERR_INVALID_ARG;
     if (overlaps(p->S_out, ns, p->S_in, ns) && p->S_out != p->S_in) return PGF_ERR_INVALID_ARG;

@@ -18,7 +18,7 @@ struct Args {
     const float *S_in;                   // entry states per sequence (NULL = zero), or
     const float *seg_in;                 // per segment
     float *S_out;
-    float *segE, *tr;                    // kSegment: end states, transitions (tr[j][i]: of entry (i, j))
+    float *segE, *tr, *trT;              // kSegment: end states, transitions, transposed ones (or NULL)
     float *saveS, *saveE;                // kSave: states entering every save-th chunk, E of every chunk
     int64_t save_per; int save;          // slots of kC * save steps of a dense sequence
     int ct, vt;                          // column tiles of a head, value tiles among them
@@ -295,7 +295,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     auto key0 = [&](int kt) { return 32 * (kt / 2) + 8 * qd + 4 * (kt & 1); };
     floatx4 S[KT];
     {
-        const float *in = MODE == kSegment ? nullptr : a.seg_in ? a.seg_in + (slot * a.Hv + h) * a.dk * a.dv
+        const float *in = MODE == kSegment ? nullptr : a.seg_in && r.len ? a.seg_in + (slot * a.Hv + h) * a.dk * a.dv
                           : a.S_in ? a.S_in + (r.n * a.Hv + h) * a.dk * a.dv : nullptr;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -542,13 +542,116 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     if (!mine) return;
     if constexpr (MODE == kSegment) {
         if (value) store_state(a.segE + (slot * a.Hv + h) * a.dk * a.dv, a.dv);
-        else if (live_col) {                       // by column: tr[col][key]
-            float *out = a.tr + (slot * a.Hv + h) * DK * DK + col * DK;
+        else if (live_col) {
+            const int64_t at = (slot * a.Hv + h) * DK * DK;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
-                if (key0(kt) < a.dk) *(floatx4 *)(out + key0(kt)) = S[kt];
+                if (key0(kt) < a.dk) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) a.tr[at + (key0(kt) + j) * DK + col] = S[kt][j];
+                    if (a.trT) *(floatx4 *)(a.trT + at + col * DK + key0(kt)) = S[kt];
+                }
         }
     } else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv, a.dv);
+}
+
+// ---------------------------------------------------------------- carry
+// The state entering each segment of a sequence, one after the other:
+// S <- M S + E with the segments' transitions M and zero-start end states E
+// (E's place receives the entry state).  BACK: the adjoint leaving each, from
+// the last to the first, with M transposed.  A block has 16 value columns of a
+// head; its four waves share the keys and pass the state's parts through LDS.
+// About 1 us a segment: its products wait for the last segment's.
+template <int DK, bool BACK>
+__device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile, char (*sS)[16 * DK * 2]) {
+    constexpr int KS = DK / 32, MT = DK / 64;      // (key tiles of a wave)
+    const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
+    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int64_t slot0 = uni(a.seqs.slot0(n, a.seg, a.seg_per));
+    const int64_t len = a.seqs.cu ? (a.seqs.bound(n + 1) > a.seqs.bound(n) ? a.seqs.bound(n + 1) - a.seqs.bound(n) : 0) : a.seqs.L;
+    const int G = (int)uni((len + a.seg - 1) / a.seg);
+    const int col = 16 * tile + c;
+    const bool on = col < a.dv;
+    const float *init = BACK ? a.dS_out : a.S_in;
+    float *E = BACK ? a.dsegE : a.segE;
+    const float *M = BACK ? a.trT : a.tr;
+    const int64_t cell = a.dk * a.dv;
+    floatx4 S[MT], e[MT];
+    Raw8<float> mr[MT][KS];
+    auto offs = [&](int m) {                       // of this lane's four keys in a state
+        const int key = 16 * (MT * w + m) + 4 * qd;
+        return on && key < a.dk ? (uint32_t)(key * a.dv + col) * 4u : kNone;
+    };
+    auto fetch = [&](int g) {
+        const int64_t at = (slot0 + (BACK ? G - 1 - g : g)) * a.Hv + h;
+        const Buf eb = make_buf((const void *)uni((int64_t)(uintptr_t)(E + at * cell)), a.dv * 4, a.dk, a.dv * 4);
+        const Buf mb = make_buf((const void *)uni((int64_t)(uintptr_t)(M + at * DK * DK)), DK * 4, a.dk, a.dk * 4);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[m][j] = raw_f<float>(load1<float>(eb, offs(m), j * eb.st));
+            const int key = 16 * (MT * w + m) + c;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                mr[m][ks] = load8<float>(mb, key < a.dk && 32 * ks + 8 * qd < a.dk ? key * mb.st + (32 * ks + 8 * qd) * 4u : kNone, 0);
+        }
+    };
+#pragma unroll
+    for (int m = 0; m < MT; ++m) S[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    if (init) {
+        const Buf ib = make_buf((const void *)uni((int64_t)(uintptr_t)(init + (n * a.Hv + h) * cell)), a.dv * 4, a.dk, a.dv * 4);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) S[m][j] = raw_f<float>(load1<float>(ib, offs(m), j * ib.st));
+    }
+    if (G > 0) fetch(0);
+    for (int g = 0; g < G; ++g) {
+        const int64_t at = (slot0 + (BACK ? G - 1 - g : g)) * a.Hv + h;
+        char *buf = &sS[3 * (g & 1)][0];
+        floatx4 acc[MT];
+        Frag<3> mf[MT][KS];
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            bf16x4 x[3];
+            split4<3>(S[m], x);
+            const int key = 16 * (MT * w + m) + 4 * qd;
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *(bf16x4 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, key / 8) + 2 * (key & 4)] = x[p];
+            acc[m] = e[m];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) mf[m][ks] = raw_frag<3>(mr[m][ks]);
+        }
+        const Buf eb = make_buf((const void *)uni((int64_t)(uintptr_t)(E + at * cell)), a.dv * 4, a.dk, a.dv * 4);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) store1<float>(eb, offs(m), j * eb.st, S[m][j]);
+        if (g + 1 < G) fetch(g + 1);
+        lds_barrier();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            Frag<3> sf;
+#pragma unroll
+            for (int p = 0; p < 3; ++p) sf.p[p] = *(const bf16x8 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, 4 * ks + qd)];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[m] = mfma_parts<3, 3>(mf[m][ks], sf, acc[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) S[m] = acc[m];
+    }
+}
+
+// BOTH: the adjoint's carry beside the state's (blockIdx.y).
+template <int DK, bool BOTH>
+__global__ __launch_bounds__(256) void k_gdr_carry(Args a) {
+    __shared__ __align__(16) char sS[6][16 * DK * 2];      // two states of three parts, by column
+    const int64_t nh = blockIdx.x / a.vt;
+    const int tile = (int)(blockIdx.x - nh * a.vt);
+    const int64_t n = nh / a.Hv;
+    const int h = (int)(nh - n * a.Hv);
+    if (BOTH && blockIdx.y) carry<DK, true>(a, n, h, tile, sS);
+    else carry<DK, false>(a, n, h, tile, sS);
 }
 
 }  // namespace gdr

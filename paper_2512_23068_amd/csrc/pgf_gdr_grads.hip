@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     auto key0 = [&](int kt) { return 32 * (kt / 2) + 8 * qd + 4 * (kt & 1); };
     floatx4 S[KT];                                 // the adjoint
     {
-        const float *in = MODE == kBackSegment ? nullptr : a.dseg_in ? a.dseg_in + (slot * a.Hv + h) * a.dk * a.dv
+        const float *in = MODE == kBackSegment ? nullptr : a.dseg_in && r.len ? a.dseg_in + (slot * a.Hv + h) * a.dk * a.dv
                           : a.dS_out ? a.dS_out + (r.n * a.Hv + h) * a.dk * a.dv : nullptr;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -635,6 +635,24 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
         hipLaunchKernelGGL((k_gdr_prep<T, DK, 3>), dim3((unsigned)((items + kPrepWaves - 1) / kPrepWaves)),
                            dim3(64 * kPrepWaves), 0, st, a, pl.chunk_slots);
     }
+    if (pl.seg) {
+        {
+            Args s = a;
+            s.ct = a.vt + (int)((pl.dk + 15) / 16);
+            const uint32_t n = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
+            Timed tm(1, st);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(n), dim3(256), 0, st, s, n);
+        }
+        {
+            const uint32_t n = (uint32_t)(pl.seg_slots * pl.Hv * ((a.vt + 3) / 4));
+            Timed tm(1, st);
+            hipLaunchKernelGGL((k_gdr_back<T, DK, kBackSegment>), dim3(n), dim3(256), 0, st, a, n);
+        }
+        Timed tm(2, st);
+        hipLaunchKernelGGL((k_gdr_carry<DK, true>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt), 2), dim3(256), 0, st, a);
+        a.seg_in = a.segE;
+        a.dseg_in = a.dsegE;
+    }
     const uint32_t blocks = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
     if (items) {
         Timed tm(1, st);
@@ -700,6 +718,7 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     a.grads = 1;
     a.segE = (float *)(ws + pl.segE);
     a.tr = (float *)(ws + pl.tr);
+    a.trT = (float *)(ws + pl.trT);
     a.S_in = p->S_in;
     a.dS_out = p->dS_out;
     a.dS_in = p->dS_in;

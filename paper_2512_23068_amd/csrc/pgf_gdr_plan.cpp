@@ -61,6 +61,35 @@ bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
 
 namespace gdr {
 
+namespace {
+
+// Steps per segment, 0 = not cut.  A wave takes 16 columns of one head through a
+// chunk of 32 steps in about 2 us while it has a SIMD to itself, and the GPU
+// (1024 SIMDs) completes one such piece per 1.8 us and SIMD when it is full.
+// Cutting costs the zero-start end states and the transitions (dk more columns,
+// without outputs: 3/4 of the work a column) on top, and the carry, one step of
+// about 1 us after the other.  So the sequences are cut when all that, spread
+// over the GPU, takes less than the longest sequence's chunks in a row; into as
+// many segments as give the first pass about 4 waves a SIMD, fewer where the
+// carry would take longer than a segment.
+int64_t default_seg(const Plan &q, bool packed) {
+    const int64_t vt = cdiv(q.dv, 16), kt = cdiv(q.dk, 16);
+    const int64_t total = cdiv(packed ? q.L : q.B * q.L, kC);
+    // Packed lengths are on the device: the longest is taken as four times the mean.
+    const int64_t longest = cdiv(packed ? std::min(q.L, 4 * q.L / q.nseq) : q.L, kC);
+    const double seq = (double)longest * std::max(1.0, 0.9 * (double)(q.nseq * q.Hv * vt) / 1024.0);
+    const int64_t waves = q.nseq * q.Hv * (vt + kt);
+    int64_t G = std::max<int64_t>(1, 4096 / waves);
+    while (G > 2 && G * G > 4 * longest) G = G * 3 / 4;
+    if (G < 2) return 0;
+    const double seg = 0.9 * (double)total * (double)q.Hv * (1.75 * (double)vt + 0.75 * (double)kt) / 1024.0 + 0.5 * (double)G + 10.0;
+    if (seg >= seq) return 0;
+    const int64_t unit = kSuper * kC;
+    return std::max<int64_t>(4 * unit, cdiv(cdiv(longest * kC, G), unit) * unit);
+}
+
+}  // namespace
+
 int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     if (!p || !out) return PGF_ERR_INVALID_ARG;
     Plan q{};
@@ -95,7 +124,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     q.chunk_slots = p->n_seqs ? q.L / kC + p->n_seqs : q.B * q.chunks_per;
     if (q.chunk_slots * q.Hv > kMaxBlocks / col_blocks || q.nseq * q.Hv > kMaxBlocks / col_blocks)
         return PGF_ERR_UNSUPPORTED;
-    q.seg = p->seg_len > 0 ? p->seg_len : 0;
+    q.seg = p->seg_len > 0 ? p->seg_len : p->seg_len < 0 ? 0 : default_seg(q, p->n_seqs > 0);
     if (q.seg >= q.L) q.seg = 0;
     q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
     q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
@@ -108,7 +137,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     ok = ok && section(&q.total, &q.segE, ns, cell) && section(&q.total, &q.tr, ns, cell_tr);
     ok = ok && section(&q.total, &q.S, nu, cell) && section(&q.total, &q.dS, nu, cell);
     ok = ok && section(&q.total, &q.u, nc, q.Hv * kC * q.dv * 4) && section(&q.total, &q.du, nc, q.Hv * kC * q.dv * 4);
-    ok = ok && section(&q.total, &q.dseg, grads ? ns : 0, cell);
+    ok = ok && section(&q.total, &q.trT, grads ? ns : 0, cell_tr) && section(&q.total, &q.dseg, grads ? ns : 0, cell);
     if (!ok) return PGF_ERR_UNSUPPORTED;
     q.total = std::max<size_t>(q.total, 256);
     *out = q;

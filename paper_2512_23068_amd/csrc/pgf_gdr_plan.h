@@ -24,6 +24,7 @@ constexpr int64_t kImgBytes = 2048;  // a 32 x 32 matrix of bf16
 //   S     [super slots][Hv][dk][dv]           state entering every kSuper chunks
 //   dS    [super slots][Hv][dk][dv]           its adjoint leaving them
 //   u, du [chunk slots][Hv][32][dv]           E and its adjoint of each chunk
+//   trT   [segment slots][Hv][DK][DK]         tr transposed
 //   dseg  [segment slots][Hv][dk][dv]         as seg, of the adjoint
 struct Plan {
     int64_t B, Hk, Hv, L, dk, dv, nseq;
@@ -33,7 +34,7 @@ struct Plan {
     int64_t seg_slots, segs_per;
     int64_t super_slots, supers_per;     // slots of kSuper * kC steps
     int64_t rec_bytes;           // of one chunk's record
-    size_t rec, segE, tr, S, dS, u, du, dseg, total;
+    size_t rec, segE, tr, S, dS, u, du, trT, dseg, total;
 };
 
 // Validates sizes, types and strides, not pointers.  step: of pgf_gdr_step.

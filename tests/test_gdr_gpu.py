@@ -208,3 +208,33 @@ def test_prompt_then_tokens(dtype):
     check("o", got, ro, TOL[dtype])
     check("S", S, rS, TOL[F32])
     check("whole", whole, ro, TOL[dtype])
+
+
+@pytest.mark.parametrize("dtype,dk,dv", [(F32, 64, 72), (BF16, 128, 40), (F32, 104, 128), (BF16, 24, 64)])
+def test_segments(dtype, dk, dv):
+    """Sequences cut into segments, the last one short, dense and packed, with
+    sequences shorter than a segment and empty ones."""
+    c, d = make(2, 1, 2, 330, dk, dv, dtype, seed=14, g_scale=0.02)
+    S0 = torch.randn(2, 2, dk, dv, generator=torch.Generator().manual_seed(9))
+    ro, rS = ref.scan(*c, dk ** -0.5, S0)
+    for seg in (-1, 64, 128):
+        o, S = binding.gdr_scan(*d, S_in=S0.to(DEV), return_state=True, seg_len=seg)
+        check(f"o seg {seg}", o, ro, TOL[dtype])
+        check(f"S seg {seg}", S, rS, TOL[F32])
+    cu = [0, 200, 200, 231, 329, 330]
+    c, d = make(1, 1, 2, 330, dk, dv, dtype, seed=15, g_scale=0.02)
+    S0 = torch.randn(5, 2, dk, dv, generator=torch.Generator().manual_seed(9))
+    want = ref.packed(lambda *a: ref.scan(*a[:5], dk ** -0.5, a[5]), cu, c, [S0])
+    o, S = binding.gdr_scan(*d, S_in=S0.to(DEV), return_state=True, seg_len=64,
+                            cu_seqlens=torch.tensor(cu, device=DEV, dtype=torch.int32))
+    check("packed o", o, torch.cat([w[0] for w in want], 2), TOL[dtype])
+    check("packed S", S, torch.cat([w[1] for w in want]), TOL[F32])
+
+
+def test_default_segments():
+    """A long sequence of one head is cut by default."""
+    c, d = make(1, 1, 1, 3000, 64, 16, F32, seed=16, g_scale=0.01)
+    o, S = binding.gdr_scan(*d, return_state=True)
+    ro, rS = ref.scan(*c, 0.125)
+    check("o", o, ro, TOL[F32])
+    check("S", S, rS, TOL[F32])

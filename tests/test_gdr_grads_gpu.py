@@ -143,3 +143,24 @@ def test_grads_into_one_array():
     got = binding.gdr_grads(*d, do, out=parts)
     assert all(g is p for g, p in zip(got, parts))
     assert all(torch.equal(x, y) for x, y in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype,dk,dv", [(F32, 64, 72), (BF16, 128, 40), (F32, 104, 128)])
+def test_grads_segments(dtype, dk, dv):
+    """Segments, the last one short, dense and packed with empty sequences."""
+    c, d = make(2, 1, 2, 330, dk, dv, dtype, seed=14, g_scale=0.02)
+    gen = torch.Generator().manual_seed(4)
+    S0, dS1 = (torch.randn(2, 2, dk, dv, generator=gen) * 0.5 for _ in range(2))
+    do = torch.randn(2, 2, 330, dv, generator=gen).to(dtype)
+    want = reference(c, do, dk ** -0.5, S0, dS1)
+    for seg in (-1, 64, 128):
+        print("segments of", seg, flush=True)
+        compare(binding.gdr_grads(*d, do.to(DEV), S_in=S0.to(DEV), dS_out=dS1.to(DEV), seg_len=seg), want, dtype)
+    cu = [0, 200, 200, 231, 329, 330]
+    c, d = make(1, 1, 2, 330, dk, dv, dtype, seed=15, g_scale=0.02)
+    S0, dS1 = (torch.randn(5, 2, dk, dv, generator=gen) * 0.5 for _ in range(2))
+    do = torch.randn(1, 2, 330, dv, generator=gen).to(dtype)
+    got = binding.gdr_grads(*d, do.to(DEV), S_in=S0.to(DEV), dS_out=dS1.to(DEV), seg_len=64,
+                            cu_seqlens=torch.tensor(cu, device=DEV, dtype=torch.int32))
+    parts = ref.packed(lambda *a: reference(a[:5], a[5], dk ** -0.5, a[6], a[7]), cu, (*c, do), [S0, dS1])
+    compare(got, [torch.cat([p[i] for p in parts], 2) for i in range(5)] + [torch.cat([p[5] for p in parts])], dtype)
