@@ -35,16 +35,20 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // compiler must not move them across this.
 __device__ __forceinline__ void wave_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
-// Block number -> work item so that neighbours in the work order (column
-// blocks of one head, which read the same keys) run on one of the 8 XCDs and
-// share its L2; the hardware deals blocks to the XCDs in turn.
-__device__ __forceinline__ uint32_t xcd_order(uint32_t b, uint32_t n) {
-    const uint32_t per = n / 8, rem = n % 8, x = b % 8;
-    return x * per + (x < rem ? x : rem) + b / 8;
+// Work item of a block, items in runs of `run` that read the same keys (the
+// column blocks of the value heads of one key head): a run's blocks are on one
+// of the 8 XCDs and share its L2, consecutive runs on different ones, so that a
+// long sequence's heads spread over the GPU.  The hardware deals blocks to the
+// XCDs in turn.  Items from n on (the grid is padded) are not there.
+__device__ __forceinline__ uint32_t xcd_item(uint32_t b, uint32_t run) {
+    const uint32_t x = b % 8, i = b / 8;
+    return (i / run * 8 + x) * run + i % run;
 }
-
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(__bf16 x) { return (float)x; }
+// Blocks for n items.
+inline unsigned xcd_grid(int64_t n, int64_t run) {
+    const int64_t runs = (n + run - 1) / run;
+    return (unsigned)((runs + 7) / 8 * 8 * run);
+}
 
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));

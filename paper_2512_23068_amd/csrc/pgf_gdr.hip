@@ -41,7 +41,8 @@ __global__ __launch_bounds__(256) void k_gdr_step(Args a, float *pool, int64_t n
     const int tid = threadIdx.x, cg = tid % CG, kg = tid / CG;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
     const int cb = (a.dv + CB - 1) / CB;
-    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const uint32_t item = xcd_item(blockIdx.x, (uint32_t)cb);
+    if (item >= n_items) return;
     const int64_t bh = item / cb;
     const int64_t b = bh / a.Hv;
     const int h = (int)(bh - b * a.Hv), hk = h / a.rep;
@@ -73,8 +74,8 @@ __global__ __launch_bounds__(256) void k_gdr_step(Args a, float *pool, int64_t n
     for (int64_t t = 0; t < L; ++t) {
         float kq = 0.0f;
         if (tid < DK) {
-            const float kx = tid < a.dk ? to_f(a.k.at<const T>(b, hk, t)[tid]) : 0.0f;
-            const float qx = tid < a.dk ? to_f(a.q.at<const T>(b, hk, t)[tid]) : 0.0f;
+            const float kx = tid < a.dk ? (float)a.k.at<const T>(b, hk, t)[tid] : 0.0f;
+            const float qx = tid < a.dk ? (float)a.q.at<const T>(b, hk, t)[tid] : 0.0f;
             sKQ[0][tid] = kx;
             sKQ[1][tid] = qx;
             kq = kx * qx;
@@ -207,7 +208,7 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
             s.ct = a.vt + (int)((pl.dk + 15) / 16);
             const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(items), dim3(256), 0, st, s, items);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(xcd_grid(items, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, items);
         }
         Timed tm(2, st);
         hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt)), dim3(256), 0, st, a);
@@ -215,7 +216,7 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
     }
     const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
     Timed tm(3, st);
-    hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut>), dim3(items), dim3(256), 0, st, a, items);
+    hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut>), dim3(xcd_grid(items, (a.ct + 3) / 4 * a.rep)), dim3(256), 0, st, a, items);
     return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;
 }
 
@@ -226,7 +227,7 @@ int step_t(const Args &a, const Plan &pl, const pgf_gdr_params *p, hipStream_t s
 #define PGF_STEP(DK_, CB_)                                                                                         \
     {                                                                                                              \
         const uint32_t items = (uint32_t)(bh * ((pl.dv + CB_ - 1) / CB_));                                         \
-        hipLaunchKernelGGL((k_gdr_step<T, DK_, CB_>), dim3(items), dim3(256), 0, st, a, p->S_pool, p->pool,        \
+        hipLaunchKernelGGL((k_gdr_step<T, DK_, CB_>), dim3(xcd_grid(items, (pl.dv + CB_ - 1) / CB_)), dim3(256), 0, st, a, p->S_pool, p->pool,        \
                            p->slots, pl.L, items);                                                                 \
     }
     // 128 columns a block once these fill the GPU, 32 before (four times the

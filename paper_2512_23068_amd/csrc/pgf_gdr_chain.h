@@ -269,7 +269,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
     const int cb = (a.ct + 3) / 4;                 // blocks of a head
-    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const uint32_t item = xcd_item(blockIdx.x, (uint32_t)(cb * a.rep));
+    if (item >= n_items) return;
     const int64_t sh = item / cb;
     const int tile = (int)(item - sh * cb) * 4 + w;
     const int64_t slot = sh / a.Hv;

@@ -45,7 +45,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
     const int cb = (a.vt + 3) / 4;
-    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const uint32_t item = xcd_item(blockIdx.x, (uint32_t)(cb * a.rep));
+    if (item >= n_items) return;
     const int64_t sh = item / cb;
     const int tile = (int)(item - sh * cb) * 4 + w;
     const int64_t slot = sh / a.Hv;
@@ -323,13 +324,13 @@ struct OuterLds {
 };
 
 template <typename T, int DK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1))) void k_gdr_outer(Args a, uint32_t n_items) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_gdr_outer(Args a, uint32_t n_items) {
     constexpr int P = sizeof(T) == 2 ? 1 : 3;
     constexpr int KT = DK / 16, SU = DK / 64, KU = kRun * DK / 8 / 256;
     __shared__ OuterLds<T, DK> lds;
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
-    const uint32_t item = xcd_order(blockIdx.x, n_items);
+    const uint32_t item = blockIdx.x;
     const int64_t sslot = item / a.Hk;
     const int hk = (int)(item - sslot * a.Hk);
     const Rows r = a.seqs.of(sslot, kRun, a.save_per);
@@ -641,12 +642,12 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
             s.ct = a.vt + (int)((pl.dk + 15) / 16);
             const uint32_t n = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(n), dim3(256), 0, st, s, n);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(xcd_grid(n, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, n);
         }
         {
             const uint32_t n = (uint32_t)(pl.seg_slots * pl.Hv * ((a.vt + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_back<T, DK, kBackSegment>), dim3(n), dim3(256), 0, st, a, n);
+            hipLaunchKernelGGL((k_gdr_back<T, DK, kBackSegment>), dim3(xcd_grid(n, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, n);
         }
         Timed tm(2, st);
         hipLaunchKernelGGL((k_gdr_carry<DK, true>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt), 2), dim3(256), 0, st, a);
@@ -656,11 +657,11 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
     const uint32_t blocks = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
     if (items) {
         Timed tm(1, st);
-        hipLaunchKernelGGL((k_gdr_chain<T, DK, kSave>), dim3(blocks), dim3(256), 0, st, a, blocks);
+        hipLaunchKernelGGL((k_gdr_chain<T, DK, kSave>), dim3(xcd_grid(blocks, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, blocks);
     }
     {
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_back<T, DK, kBack>), dim3(blocks), dim3(256), 0, st, a, blocks);
+        hipLaunchKernelGGL((k_gdr_back<T, DK, kBack>), dim3(xcd_grid(blocks, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, blocks);
     }
     if (items) {
         Timed tm(3, st);

@@ -8,7 +8,7 @@ namespace pgf {
 
 namespace {
 
-constexpr int64_t kMaxBlocks = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxBlocks = int64_t(1) << 30;
 constexpr int64_t kMaxHeads = int64_t(1) << 16, kMaxBatch = int64_t(1) << 24, kMaxLen = int64_t(1) << 32;
 constexpr int64_t kMaxStride = int64_t(1) << 44;
 constexpr int64_t kMaxStep = (int64_t(1) << 24) - 16;      // bytes from step to step
@@ -113,7 +113,8 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
     q.DK = q.dk <= 64 ? 64 : 128;
     q.nseq = p->n_seqs ? p->n_seqs : q.B;
-    const int64_t col_blocks = cdiv(q.dv, 16) + q.DK / 16;      // an upper bound of the blocks of one head
+    // An upper bound of the blocks of one head; grids are padded by less than 8 key heads.
+    const int64_t col_blocks = cdiv(q.dv, 16) + q.DK / 16;
     if (step) {
         if (p->pool < 0 || p->pool > kMaxLen) return PGF_ERR_INVALID_ARG;
         if (q.B * q.Hv > kMaxBlocks / col_blocks) return PGF_ERR_UNSUPPORTED;
