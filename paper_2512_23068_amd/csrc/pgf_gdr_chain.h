@@ -28,6 +28,7 @@ struct Args {
     float *dS_in;                        // dl/dS entering sequences
     float *dsegE;                        // kBackSegment: adjoint at the segments' starts, from zero
     float *saveD, *saveU;                // kBack: adjoint of the state leaving every save chunks, dl/dE of every chunk
+    float *acc;                          // sums of dq over value heads
     float *dg, *dbeta;                   // dense [B][Hv][L]
 };
 

@@ -298,326 +298,398 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
 // ---------------------------------------------------------------- outer
 // A block takes 64 steps of one key head; wave w their tile of 16 steps 16 w ..
-// as columns of every product, and all keys as rows, so that the sums over
-// keys (dbeta, dG) stay in a wave.  Phase one runs over the value columns, 32
-// at a time through LDS in three parts: z = dS1 E, y = S0 dE, S0 dO, and the
-// 64 x 64 products of E, dE and dO, each in the orientation its next product
-// wants it as operand.  Phase two adds the products with K and Q.
+// as columns of every product, and all keys as rows, so that the sums over keys
+// (dbeta, dG) stay in a wave.  Per value head it goes through two sides: side 0
+// has what reads the state (y, S0 dO and the products with earlier steps: dq,
+// r), side 1 what writes it (z and the products with later steps: w).  Phase one
+// of a side runs over the value columns, 32 at a time through LDS in three
+// parts: the products with S0 (or dS1), and the 64 x 64 products of E, dE and
+// dO in the orientation the next product wants them as operand.  Phase two adds
+// the products with K and Q.  One side after the other needs half the registers
+// and LDS of both at once, so that two blocks share a CU and one computes while
+// the other loads.
 // Bound by the matrix cores (2850 instructions a block and head at 128 x 128)
 // and by the reads of S0 and dS1.
 constexpr int kRun = kC * kSuper;
+constexpr double kLog2e = 1.4426950408889634;
 
 template <typename T, int DK>
 struct OuterLds {
     static constexpr int P = sizeof(T) == 2 ? 1 : 3;
     union {
         struct {
-            __align__(16) char S0[3][DK * 64], S1[3][DK * 64];       // rows of 32 value columns
+            __align__(16) char S[3][DK * 64];      // rows of 32 value columns
             __align__(16) char E[3][kRun * 64], dE[3][kRun * 64], dO[P][kRun * 64];
         } v;
         struct {
             __align__(16) char K[P][kRun * DK * 2], Q[P][kRun * DK * 2];
         } k;
     };
-    double G[kRun];
-    float be[kRun], dG[kRun], kz[kRun], dot[4];
+    double G[kRun];                                // sums of g, in powers of two
+    float be[kRun], dG[2][kRun], kz[kRun], dot[4];
 };
 
-template <typename T, int DK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_gdr_outer(Args a, uint32_t n_items) {
+// One side of one value head.  accq, acck: f32 sums on their way over the value
+// heads (and dk's from side to side), in the workspace: each place is written
+// and read by one lane.  In registers they left too few for the products'
+// operands.
+template <typename T, int DK, int SIDE>
+__device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, const Rows &r, int64_t t0, int live,
+                                           int64_t slot0, int64_t sslot, int hk, int vh, int w, float *accq, float *acck) {
     constexpr int P = sizeof(T) == 2 ? 1 : 3;
-    constexpr int KT = DK / 16, SU = DK / 64, KU = kRun * DK / 8 / 256;
-    __shared__ OuterLds<T, DK> lds;
-    const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
-    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
-    const uint32_t item = blockIdx.x;
-    const int64_t sslot = item / a.Hk;
-    const int hk = (int)(item - sslot * a.Hk);
-    const Rows r = a.seqs.of(sslot, kRun, a.save_per);
-    if (r.unit0 >= r.len) return;                  // uniform over the block
-    const int live = (int)uni(r.len - r.unit0 < kRun ? r.len - r.unit0 : kRun);
-    const int64_t t0 = uni(r.lo + r.unit0);
-    const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
-    const int tok = 16 * w + c;                    // this lane's step
-
-    floatx4 dqs[KT], dks[KT];                      // sums over the value heads
+    constexpr int KT = DK / 16, KU = kRun * DK / 8 / 256;
+    constexpr int SU = DK / 64;                    // 8-column units of S0 (dS1) a thread stages
+    const int h = hk * a.rep + vh, lane = threadIdx.x % 64;
+    // The lane's place, hidden from the compiler's motion of what does not
+    // change out of the loop: the LDS addresses of both phases, kept over the
+    // loop, took a hundred registers more than there are.
+    int c = lane % 16, qd = lane / 16, tid = threadIdx.x;
+    asm volatile("" : "+v"(c), "+v"(qd), "+v"(tid));
+    // ---- phase one
+    floatx4 x1[KT], x2[SIDE ? 1 : KT], d1[4], d2[4];      // side 0: y, S0 dO; side 1: z
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) dqs[kt] = dks[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int vh = 0; vh < a.rep; ++vh) {
-        const int h = hk * a.rep + vh;
-        lds_barrier();                             // (the last head's reads)
-        if (w == 0) {
-            float g = 0.0f, be = 0.0f;
-            if (lane < live) {
-                g = *a.g.at<const float>(r.b, h, t0 + lane);
-                be = *a.beta.at<const float>(r.b, h, t0 + lane);
-                g = g < -200.0f ? -200.0f : g;
-            }
-            double G = g;
+    for (int kt = 0; kt < KT; ++kt) {
+        x1[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (SIDE == 0) x2[kt] = x1[kt];
+    }
 #pragma unroll
-            for (int m = 1; m < 64; m *= 2) {
-                const double o = __shfl_up(G, m, 64);
-                if (lane >= m) G += o;
-            }
-            lds.G[lane] = G;
-            lds.be[lane] = be;
+    for (int i = 0; i < 4; ++i) d1[i] = d2[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+    float ss = 0.0f;                           // <dS1, S0>
+    const int64_t cell = (sslot * a.Hv + h) * (int64_t)(a.dk * a.dv);
+    const Buf s0b = make_buf((const void *)uni((int64_t)(uintptr_t)((SIDE ? a.saveD : a.saveS) + cell)), a.dv * 4, a.dk, a.dv * 4);
+    const Buf s1b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveS + cell)), a.dv * 4, a.dk, a.dv * 4);
+    const Buf gb = make_buf(row_ptr<T>(a.go, r.b, h, t0), (uint32_t)a.go.st * sizeof(T), live, a.dv * (int)sizeof(T));
+    const int eu = tid % 4, er = tid / 4;      // unit and row (of S0, E, dE and dO)
+    const bool elive = er < live;
+    const int64_t eat = ((slot0 + (elive ? er / kC : 0)) * a.Hv + h) * (int64_t)(kC * a.dv) + (elive ? er % kC * a.dv : 0);
+    Raw8<float> r0[SU], r1[SIDE ? SU : 1], re, rd;      // (side 1: S0 too, for <dS1, S0>)
+    Raw8<T> rg;
+    auto fetch = [&](int v0) {
+        const bool con = v0 + 8 * eu < a.dv;   // this thread's columns are there
+        const uint32_t vc = (uint32_t)(v0 + 8 * eu);
+#pragma unroll
+        for (int i = 0; i < SU; ++i) {
+            const uint32_t at = con ? (uint32_t)(er + 64 * i) * (a.dv * 4u) + vc * 4u : kNone;
+            r0[i] = load8<float>(s0b, at, 0);
+            if constexpr (SIDE == 1) r1[i] = load8<float>(s1b, at, 0);
         }
-        // ---- phase one
-        floatx4 z[KT], y[KT], o[KT], d1t[4], d1s[4], d2t[4], d2s[4];
+        const float *ep = a.saveE + eat + (con ? vc : 0), *dp = a.saveU + eat + (con ? vc : 0);
+        re.x = *(const uintx4 *)ep;
+        re.y = *(const uintx4 *)(ep + 4);
+        rd.x = *(const uintx4 *)dp;
+        rd.y = *(const uintx4 *)(dp + 4);
+        rg = load8<T>(gb, con ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
+    };
+    fetch(0);
+    lds_barrier();                             // (the last side's reads)
+    if (SIDE == 0 && w == 3) {
+        float g = 0.0f, be = 0.0f;
+        if (lane < live) {
+            g = *a.g.at<const float>(r.b, h, t0 + lane);
+            be = *a.beta.at<const float>(r.b, h, t0 + lane);
+            g = g < -200.0f ? -200.0f : g;
+        }
+        double G = g;
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) z[kt] = y[kt] = o[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d1t[i] = d1s[i] = d2t[i] = d2s[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-        float ss = 0.0f;                           // <dS1, S0>
-        const int64_t cell = (sslot * a.Hv + h) * (int64_t)(a.dk * a.dv);
-        const Buf s0b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveS + cell)), a.dv * 4, a.dk, a.dv * 4);
-        const Buf s1b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveD + cell)), a.dv * 4, a.dk, a.dv * 4);
-        const Buf gb = make_buf(row_ptr<T>(a.go, r.b, h, t0), (uint32_t)a.go.st * sizeof(T), live, a.dv * (int)sizeof(T));
-        const int er = tid / 4, eu = tid % 4;      // row and unit of E, dE and dO
-        const bool elive = er < live;
-        const int64_t eat = ((slot0 + (elive ? er / kC : 0)) * a.Hv + h) * (int64_t)(kC * a.dv) + (elive ? er % kC * a.dv : 0);
-        Raw8<float> r0[SU], r1[SU], re, rd;
-        Raw8<T> rg;
-        bool con;                                  // this thread's columns are there
-        auto fetch = [&](int v0) {
-            con = v0 + 8 * eu < a.dv;
-            const uint32_t vc = (uint32_t)(v0 + 8 * eu);
-#pragma unroll
-            for (int i = 0; i < SU; ++i) {
-                const uint32_t at = con ? (uint32_t)(er + 64 * i) * (a.dv * 4u) + vc * 4u : kNone;
-                r0[i] = load8<float>(s0b, at, 0);
-                r1[i] = load8<float>(s1b, at, 0);
+        for (int m = 1; m < 64; m *= 2) {
+            const double o = __shfl_up(G, m, 64);
+            if (lane >= m) G += o;
+        }
+        lds.G[lane] = G * kLog2e;
+        lds.be[lane] = be;
+    }
+    for (int v0 = 0; v0 < a.dv; v0 += 32) {
+        if (v0) lds_barrier();                 // the last columns' reads
+        {
+            const uint32_t at = unit_off<32>(er, eu);
+            Raw8<float> me = re, md = rd;
+            if (!(v0 + 8 * eu < a.dv && elive)) {
+                me.x = me.y = uintx4{};
+                md.x = md.y = uintx4{};
             }
-            const float *ep = a.saveE + eat + (con ? vc : 0), *dp = a.saveU + eat + (con ? vc : 0);
-            re.x = *(const uintx4 *)ep;
-            re.y = *(const uintx4 *)(ep + 4);
-            rd.x = *(const uintx4 *)dp;
-            rd.y = *(const uintx4 *)(dp + 4);
-            rg = load8<T>(gb, con ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
-        };
-        fetch(0);
-        for (int v0 = 0; v0 < a.dv; v0 += 32) {
-            if (v0) lds_barrier();                 // the last columns' reads
-            {
-                const uint32_t at = unit_off<32>(er, eu);
-                if (!(con && elive)) {
-                    re.x = re.y = uintx4{};
-                    rd.x = rd.y = uintx4{};
-                }
-                const Frag<3> fe = raw_frag<3>(re), fd = raw_frag<3>(rd);
-                const Frag<P> fg = raw_frag<P>(rg);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    *(bf16x8 *)&lds.v.E[p][at] = fe.p[p];
-                    *(bf16x8 *)&lds.v.dE[p][at] = fd.p[p];
-                }
-#pragma unroll
-                for (int p = 0; p < P; ++p) *(bf16x8 *)&lds.v.dO[p][at] = fg.p[p];
-#pragma unroll
-                for (int i = 0; i < SU; ++i) {
-                    const uint32_t sa = unit_off<32>(er + 64 * i, eu);
-                    const Frag<3> f0 = raw_frag<3>(r0[i]), f1 = raw_frag<3>(r1[i]);
-#pragma unroll
-                    for (int p = 0; p < 3; ++p) {
-                        *(bf16x8 *)&lds.v.S0[p][sa] = f0.p[p];
-                        *(bf16x8 *)&lds.v.S1[p][sa] = f1.p[p];
-                    }
-                    const floatx4 x0 = __builtin_bit_cast(floatx4, r0[i].x), x1 = __builtin_bit_cast(floatx4, r1[i].x);
-                    const floatx4 y0 = __builtin_bit_cast(floatx4, r0[i].y), y1 = __builtin_bit_cast(floatx4, r1[i].y);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) ss = fmaf(x0[j], x1[j], fmaf(y0[j], y1[j], ss));
-                }
-            }
-            fetch(v0 + 32 < a.dv ? v0 + 32 : v0);
-            lds_barrier();
-            Frag<3> ew, dw;                        // this wave's steps as columns
-            Frag<P> gw;
-            const uint32_t wa = unit_off<32>(16 * w + c, qd);
+            const Frag<3> fe = raw_frag<3>(me), fd = raw_frag<3>(md);
+            const Frag<P> fg = raw_frag<P>(rg);
 #pragma unroll
             for (int p = 0; p < 3; ++p) {
-                ew.p[p] = *(const bf16x8 *)&lds.v.E[p][wa];
-                dw.p[p] = *(const bf16x8 *)&lds.v.dE[p][wa];
+                *(bf16x8 *)&lds.v.E[p][at] = fe.p[p];
+                *(bf16x8 *)&lds.v.dE[p][at] = fd.p[p];
             }
 #pragma unroll
-            for (int p = 0; p < P; ++p) gw.p[p] = *(const bf16x8 *)&lds.v.dO[p][wa];
+            for (int p = 0; p < P; ++p) *(bf16x8 *)&lds.v.dO[p][at] = fg.p[p];
+#pragma unroll
+            for (int i = 0; i < SU; ++i) {
+                const Frag<3> f = raw_frag<3>(r0[i]);
+#pragma unroll
+                for (int p = 0; p < 3; ++p) *(bf16x8 *)&lds.v.S[p][unit_off<32>(er + 64 * i, eu)] = f.p[p];
+                if constexpr (SIDE == 1) {
+                    const floatx4 a0 = __builtin_bit_cast(floatx4, r0[i].x), a1 = __builtin_bit_cast(floatx4, r1[i].x);
+                    const floatx4 b0 = __builtin_bit_cast(floatx4, r0[i].y), b1 = __builtin_bit_cast(floatx4, r1[i].y);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ss = fmaf(a0[j], a1[j], fmaf(b0[j], b1[j], ss));
+                }
+            }
+        }
+        fetch(v0 + 32 < a.dv ? v0 + 32 : v0);
+        lds_barrier();
+        // (each operand is read one tile ahead, and no further: more take registers)
+        const uint32_t wa = unit_off<32>(16 * w + c, qd);      // this wave's steps as columns
+        Frag<3> f[2];
+        auto rd_s = [&](int kt) {
+#pragma unroll
+            for (int p = 0; p < 3; ++p) f[kt & 1].p[p] = *(const bf16x8 *)&lds.v.S[p][unit_off<32>(16 * kt + c, qd)];
+        };
+        Frag<3> xw;                            // dE or E
+        Frag<P> gw;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) xw.p[p] = *(const bf16x8 *)&(SIDE ? lds.v.E : lds.v.dE)[p][wa];
+#pragma unroll
+        for (int p = 0; p < P; ++p) gw.p[p] = *(const bf16x8 *)&lds.v.dO[p][wa];
+        rd_s(0);
+        if constexpr (SIDE == 0) {
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                Frag<3> f0, f1;
-                const uint32_t at = unit_off<32>(16 * kt + c, qd);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    f0.p[p] = *(const bf16x8 *)&lds.v.S0[p][at];
-                    f1.p[p] = *(const bf16x8 *)&lds.v.S1[p][at];
-                }
-                z[kt] = mfma_parts<3, 3>(f1, ew, z[kt]);
-                y[kt] = mfma_parts<3, 3>(f0, dw, y[kt]);
-                o[kt] = mfma_parts<3, P>(f0, gw, o[kt]);
+                if (kt + 1 < KT) rd_s(kt + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                x1[kt] = mfma_parts<3, 3>(f[kt & 1], xw, x1[kt]);
+                x2[kt] = mfma_parts<3, P>(f[kt & 1], gw, x2[kt]);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                Frag<3> fe, fd;
+                __builtin_amdgcn_sched_barrier(0);
+                Frag<3> fe;
+#pragma unroll
+                for (int p = 0; p < 3; ++p) fe.p[p] = *(const bf16x8 *)&lds.v.E[p][unit_off<32>(16 * i + c, qd)];
+                d1[i] = mfma_parts<3, P>(fe, gw, d1[i]);
+                d2[i] = mfma_parts<3, 3>(fe, xw, d2[i]);
+            }
+        } else {
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                if (kt + 1 < KT) rd_s(kt + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                x1[kt] = mfma_parts<3, 3>(f[kt & 1], xw, x1[kt]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                Frag<3> fd;
                 Frag<P> fg;
                 const uint32_t at = unit_off<32>(16 * i + c, qd);
-                if (i <= w) {                      // (uniform over the wave)
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) fe.p[p] = *(const bf16x8 *)&lds.v.E[p][at];
-                    d1t[i] = mfma_parts<3, P>(fe, gw, d1t[i]);
-                    d2t[i] = mfma_parts<3, 3>(fe, dw, d2t[i]);
-                }
-                if (i >= w) {
+                for (int p = 0; p < P; ++p) fg.p[p] = *(const bf16x8 *)&lds.v.dO[p][at];
 #pragma unroll
-                    for (int p = 0; p < 3; ++p) fd.p[p] = *(const bf16x8 *)&lds.v.dE[p][at];
-#pragma unroll
-                    for (int p = 0; p < P; ++p) fg.p[p] = *(const bf16x8 *)&lds.v.dO[p][at];
-                    d1s[i] = mfma_parts<P, 3>(fg, ew, d1s[i]);
-                    d2s[i] = mfma_parts<3, 3>(fd, ew, d2s[i]);
-                }
+                for (int p = 0; p < 3; ++p) fd.p[p] = *(const bf16x8 *)&lds.v.dE[p][at];
+                d1[i] = mfma_parts<P, 3>(fg, xw, d1[i]);
+                d2[i] = mfma_parts<3, 3>(fd, xw, d2[i]);
             }
         }
-        // ---- phase two
+    }
+    // ---- phase two
+    asm volatile("" : "+v"(c), "+v"(qd), "+v"(tid));
+    const int tok = 16 * w + c;                // this lane's step
+    Raw8<T> rk[KU], rq[KU];
+    {
+        const Buf kb = make_buf(row_ptr<T>(a.k, r.b, hk, t0), (uint32_t)a.k.st * sizeof(T), live, a.dk * (int)sizeof(T));
+        const Buf qb = make_buf(row_ptr<T>(a.q, r.b, hk, t0), (uint32_t)a.q.st * sizeof(T), live, a.dk * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < KU; ++i) {
+            const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
+            rk[i] = load8<T>(kb, e < a.dk ? t * kb.st + e * (uint32_t)sizeof(T) : kNone, 0);
+            rq[i] = load8<T>(qb, e < a.dk ? t * qb.st + e * (uint32_t)sizeof(T) : kNone, 0);
+        }
+    }
+    if constexpr (SIDE == 1) {
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) ss += __shfl_xor(ss, m, 64);
         if (lane == 0) lds.dot[w] = ss;
-        lds_barrier();                             // phase one's reads
-        {
-            const Buf kb = make_buf(row_ptr<T>(a.k, r.b, hk, t0), (uint32_t)a.k.st * sizeof(T), live, a.dk * (int)sizeof(T));
-            const Buf qb = make_buf(row_ptr<T>(a.q, r.b, hk, t0), (uint32_t)a.q.st * sizeof(T), live, a.dk * (int)sizeof(T));
-            Raw8<T> rk[KU], rq[KU];
+    }
+    const double Gt = lds.G[tok], Gend = lds.G[kRun - 1];
+    const float be = lds.be[tok];
+    // decays and signs of the 64 x 64 products; what has no place is zero
 #pragma unroll
-            for (int i = 0; i < KU; ++i) {
-                const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
-                rk[i] = load8<T>(kb, e < a.dk ? t * kb.st + e * (uint32_t)sizeof(T) : kNone, 0);
-                rq[i] = load8<T>(qb, e < a.dk ? t * qb.st + e * (uint32_t)sizeof(T) : kNone, 0);
-            }
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int i = 0; i < KU; ++i) {
-                const int u = tid + 256 * i, t = u / (DK / 8);
-                const uint32_t at = unit_off<DK>(t, u % (DK / 8));
-                const Frag<P> f = raw_frag<P>(rk[i]), x = raw_frag<P>(rq[i]);
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    *(bf16x8 *)&lds.k.K[p][at] = f.p[p];
-                    *(bf16x8 *)&lds.k.Q[p][at] = x.p[p];
-                }
-            }
+        for (int j = 0; j < 4; ++j) {
+            const int row = 16 * i + 4 * qd + j;
+            const float dG = (float)(Gt - lds.G[row]);
+            const bool at = SIDE ? row >= tok : row <= tok;
+            const float e = __builtin_amdgcn_exp2f(at ? (SIDE ? -dG : dG) : 0.0f) * (SIDE ? 1.0f : lds.be[row]);
+            d1[i][j] = at ? a.scale * e * d1[i][j] : 0.0f;
+            d2[i][j] = at && row != tok ? -e * d2[i][j] : 0.0f;
         }
-        const double Gt = lds.G[tok], Gend = lds.G[kRun - 1];
-        const float eG = expf((float)Gt), out = expf((float)(Gend - Gt)), be = lds.be[tok];
-        // decays and signs of the 64 x 64 products; what has no place is zero
+    lds_barrier();                             // phase one's reads
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < KU; ++i) {
+        const int u = tid + 256 * i, t = u / (DK / 8);
+        const uint32_t at = unit_off<DK>(t, u % (DK / 8));
+        const Frag<P> f = raw_frag<P>(rk[i]), x = raw_frag<P>(rq[i]);
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+            *(bf16x8 *)&lds.k.K[p][at] = f.p[p];
+            *(bf16x8 *)&lds.k.Q[p][at] = x.p[p];
+        }
+    }
+    lds_barrier();
+    // keys 16 kt + 4 qd .. of this lane's step
+    auto row4 = [&](const char (*m)[kRun * DK * 2], int kt) {
+        floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int p = P - 1; p >= 0; --p)
+            x += __builtin_convertvector(*(const bf16x4 *)&m[p][unit_off<DK>(tok, 2 * kt + qd / 2) + 8 * (qd & 1)], floatx4);
+        return x;
+    };
+    // operand of keys 16 kt .. and the 32 steps of block b, transposed
+    auto tr = [&](const char (*m)[kRun * DK * 2], int b, int kt) {
+        Frag<P> f;
+        const int row = 32 * b + 4 * qd + c / 4, p4 = c % 4;
+        const uint32_t o0 = unit_off<DK>(row, 2 * kt + p4 / 2) + 8 * (p4 & 1);
+        const uint32_t o1 = unit_off<DK>(row + 16, 2 * kt + p4 / 2) + 8 * (p4 & 1);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            f.p[p] = __builtin_shufflevector(read_tr(&m[p][o0]), read_tr(&m[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
+        return f;
+    };
+    if constexpr (SIDE == 0) {
+        const float eG = __builtin_amdgcn_exp2f((float)Gt);
+        float qdq = 0.0f, kr = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int row = 16 * i + 4 * qd + j;
-                const float dG = (float)(Gt - lds.G[row]);
-                const float e = expf(row <= tok ? dG : -dG);         // both directions decay
-                const float br = lds.be[row];
-                d1t[i][j] = row <= tok ? a.scale * e * br * d1t[i][j] : 0.0f;
-                d2t[i][j] = row < tok ? -e * br * d2t[i][j] : 0.0f;
-                d1s[i][j] = row >= tok ? a.scale * e * d1s[i][j] : 0.0f;
-                d2s[i][j] = row > tok ? -e * d2s[i][j] : 0.0f;
+                x1[kt][j] *= -eG;
+                x2[kt][j] *= a.scale * eG;
             }
-        lds_barrier();
-        // keys 16 kt + 4 qd .. of this lane's step
-        auto row4 = [&](const char (*m)[kRun * DK * 2], int kt) {
-            floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int p = P - 1; p >= 0; --p)
-                x += __builtin_convertvector(*(const bf16x4 *)&m[p][unit_off<DK>(tok, 2 * kt + qd / 2) + 8 * (qd & 1)], floatx4);
-            return x;
-        };
-        float kz = 0.0f, qdq = 0.0f, kr = 0.0f, kw = 0.0f;
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            const floatx4 kx = row4(lds.k.K, kt);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                z[kt][j] *= out;
-                y[kt][j] *= -eG;
-                o[kt][j] *= a.scale * eG;
-                kz = fmaf(kx[j], z[kt][j], kz);
-            }
-        }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const bool early = 2 * b <= w, late = 2 * b + 1 >= w;    // (uniform over the wave)
-            const Frag<3> f1t = to_frag<3>(d1t[2 * b], d1t[2 * b + 1]), f2t = to_frag<3>(d2t[2 * b], d2t[2 * b + 1]);
-            const Frag<3> f1s = to_frag<3>(d1s[2 * b], d1s[2 * b + 1]), f2s = to_frag<3>(d2s[2 * b], d2s[2 * b + 1]);
+            if (2 * b > w) continue;           // (uniform over the wave)
+            const Frag<3> f1 = to_frag<3>(d1[2 * b], d1[2 * b + 1]), f2 = to_frag<3>(d2[2 * b], d2[2 * b + 1]);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
-                Frag<P> kf, qf;
-                const int row = 32 * b + 4 * qd + c / 4, p4 = c % 4;
-                const uint32_t o0 = unit_off<DK>(row, 2 * kt + p4 / 2) + 8 * (p4 & 1);
-                const uint32_t o1 = unit_off<DK>(row + 16, 2 * kt + p4 / 2) + 8 * (p4 & 1);
-#pragma unroll
-                for (int p = 0; p < P; ++p) {
-                    kf.p[p] = __builtin_shufflevector(read_tr(&lds.k.K[p][o0]), read_tr(&lds.k.K[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
-                    qf.p[p] = __builtin_shufflevector(read_tr(&lds.k.Q[p][o0]), read_tr(&lds.k.Q[p][o1]), 0, 1, 2, 3, 4, 5, 6, 7);
-                }
-                if (early) {
-                    o[kt] = mfma_parts<P, 3>(kf, f1t, o[kt]);
-                    y[kt] = mfma_parts<P, 3>(kf, f2t, y[kt]);
-                }
-                if (late) {
-                    z[kt] = mfma_parts<P, 3>(qf, f1s, z[kt]);
-                    z[kt] = mfma_parts<P, 3>(kf, f2s, z[kt]);
-                }
+                const Frag<P> kf = tr(lds.k.K, b, kt);
+                if (kt % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                x2[kt] = mfma_parts<P, 3>(kf, f1, x2[kt]);
+                x1[kt] = mfma_parts<P, 3>(kf, f2, x1[kt]);
             }
         }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             const floatx4 kx = row4(lds.k.K, kt), qx = row4(lds.k.Q, kt);
+            if (kt % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                kw = fmaf(kx[j], z[kt][j], kw);
-                kr = fmaf(kx[j], y[kt][j], kr);
-                qdq = fmaf(qx[j], o[kt][j], qdq);
-                dqs[kt][j] += o[kt][j];
-                dks[kt][j] += fmaf(be, z[kt][j], y[kt][j]);
+                kr = fmaf(kx[j], x1[kt][j], kr);
+                qdq = fmaf(qx[j], x2[kt][j], qdq);
+            }
+        }
+        float s = qdq + kr;
+#pragma unroll
+        for (int m = 16; m < 64; m *= 2) s += __shfl_xor(s, m, 64);
+        if (qd == 0) lds.dG[0][tok] = s;
+        T *out = tok < live ? a.dq.at<T>(r.b, hk, t0 + tok) : nullptr;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const int key = 16 * kt + 4 * qd;
+            if (key >= a.dk) continue;
+            floatx4 &aq = *(floatx4 *)(accq + tok * a.dk + key), &ak = *(floatx4 *)(acck + tok * a.dk + key);
+            ak = vh ? ak + x1[kt] : x1[kt];
+            const floatx4 v = vh ? aq + x2[kt] : x2[kt];
+            if (vh + 1 < a.rep) aq = v;
+            else if (tok < live) {
+                Raw4<T> x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x.x[j] = (T)v[j];
+                *(Raw4<T> *)(out + key) = x;
+            }
+        }
+    } else {
+        const float out = __builtin_amdgcn_exp2f((float)(Gend - Gt));
+        float kz = 0.0f, kw = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const floatx4 kx = row4(lds.k.K, kt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x1[kt][j] *= out;
+                kz = fmaf(kx[j], x1[kt][j], kz);
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (2 * b + 1 < w) continue;
+            const Frag<3> f1 = to_frag<3>(d1[2 * b], d1[2 * b + 1]), f2 = to_frag<3>(d2[2 * b], d2[2 * b + 1]);
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                if (kt % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+                x1[kt] = mfma_parts<P, 3>(tr(lds.k.Q, b, kt), f1, x1[kt]);
+                x1[kt] = mfma_parts<P, 3>(tr(lds.k.K, b, kt), f2, x1[kt]);
+            }
+        }
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const floatx4 kx = row4(lds.k.K, kt);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kw = fmaf(kx[j], x1[kt][j], kw);
+        }
+        T *dko = tok < live ? a.dk_.at<T>(r.b, hk, t0 + tok) : nullptr;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const int key = 16 * kt + 4 * qd;
+            if (key >= a.dk) continue;
+            floatx4 &ak = *(floatx4 *)(acck + tok * a.dk + key);
+            floatx4 v = ak;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = fmaf(be, x1[kt][j], v[j]);
+            if (vh + 1 < a.rep) ak = v;
+            else if (tok < live) {
+                Raw4<T> x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x.x[j] = (T)v[j];
+                *(Raw4<T> *)(dko + key) = x;
             }
         }
 #pragma unroll
         for (int m = 16; m < 64; m *= 2) {
             kz += __shfl_xor(kz, m, 64);
             kw += __shfl_xor(kw, m, 64);
-            kr += __shfl_xor(kr, m, 64);
-            qdq += __shfl_xor(qdq, m, 64);
         }
         if (qd == 0) {
-            lds.dG[tok] = qdq + kr - be * kw;
+            lds.dG[1][tok] = -be * kw;
             lds.kz[tok] = be * kz;
             if (tok < live) a.dbeta[(r.b * a.Hv + h) * a.seqs.L + t0 + tok] = kw;
         }
         lds_barrier();
-        if (w == 0) {
-            double v = lds.dG[lane], e = lds.kz[lane];
-#pragma unroll
-            for (int m = 1; m < 64; m *= 2) e += __shfl_xor(e, m, 64);
+        if (w == vh % 4) {
+            double v = (double)lds.dG[0][lane] + lds.dG[1][lane], e = lds.kz[lane];
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) {
+                e += __shfl_xor(e, m, 64);
                 const double x = __shfl_down(v, m, 64);
                 if (lane + m < 64) v += x;
             }
             const double s01 = (double)lds.dot[0] + lds.dot[1] + lds.dot[2] + lds.dot[3];
             if (lane < live)
-                a.dg[(r.b * a.Hv + h) * a.seqs.L + t0 + lane] = (float)(v + e + (double)expf((float)Gend) * s01);
+                a.dg[(r.b * a.Hv + h) * a.seqs.L + t0 + lane] =
+                    (float)(v + e + (double)__builtin_amdgcn_exp2f((float)lds.G[kRun - 1]) * s01);
         }
     }
-    if (tok >= live) return;
-    T *dq = a.dq.at<T>(r.b, hk, t0 + tok), *dk = a.dk_.at<T>(r.b, hk, t0 + tok);
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-        const int key = 16 * kt + 4 * qd;
-        if (key < a.dk) {
-            Raw4<T> x, u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x.x[j] = (T)dqs[kt][j];
-                u.x[j] = (T)dks[kt][j];
-            }
-            *(Raw4<T> *)(dq + key) = x;
-            *(Raw4<T> *)(dk + key) = u;
-        }
+}
+
+template <typename T, int DK>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_outer(Args a) {
+    __shared__ OuterLds<T, DK> lds;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t sslot = blockIdx.x / a.Hk;
+    const int hk = (int)(blockIdx.x - sslot * a.Hk);
+    const Rows r = a.seqs.of(sslot, kRun, a.save_per);
+    if (r.unit0 >= r.len) return;                  // uniform over the block
+    const int live = (int)uni(r.len - r.unit0 < kRun ? r.len - r.unit0 : kRun);
+    const int64_t t0 = uni(r.lo + r.unit0);
+    const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
+
+    float *const accq = a.acc + (sslot * a.Hk + hk) * (int64_t)(2 * kRun * a.dk), *const acck = accq + kRun * a.dk;
+    for (int vh = 0; vh < a.rep; ++vh) {
+        outer_side<T, DK, 0>(a, lds, r, t0, live, slot0, sslot, hk, vh, w, accq, acck);
+        outer_side<T, DK, 1>(a, lds, r, t0, live, slot0, sslot, hk, vh, w, accq, acck);
     }
 }
 
@@ -666,7 +738,7 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
     if (items) {
         Timed tm(3, st);
         const uint32_t n = (uint32_t)(pl.super_slots * pl.Hk);
-        hipLaunchKernelGGL((k_gdr_outer<T, DK>), dim3(n), dim3(256), 0, st, a, n);
+        hipLaunchKernelGGL((k_gdr_outer<T, DK>), dim3(n), dim3(256), 0, st, a);
     }
     return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;
 }
@@ -728,6 +800,7 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     a.saveE = (float *)(ws + pl.u);
     a.saveU = (float *)(ws + pl.du);
     a.dsegE = (float *)(ws + pl.dseg);
+    a.acc = (float *)(ws + pl.acc);
     a.save = kSuper;
     a.save_per = pl.supers_per;
     a.dg = dg;

@@ -26,6 +26,7 @@ constexpr int64_t kImgBytes = 2048;  // a 32 x 32 matrix of bf16
 //   u, du [chunk slots][Hv][32][dv]           E and its adjoint of each chunk
 //   trT   [segment slots][Hv][DK][DK]         tr transposed
 //   dseg  [segment slots][Hv][dk][dv]         as seg, of the adjoint
+//   acc   [super slots][Hk][2][64][dk]        sums of dq and dk over value heads
 struct Plan {
     int64_t B, Hk, Hv, L, dk, dv, nseq;
     int DK;                      // d_key padded to the kernels' 64 or 128
@@ -34,7 +35,7 @@ struct Plan {
     int64_t seg_slots, segs_per;
     int64_t super_slots, supers_per;     // slots of kSuper * kC steps
     int64_t rec_bytes;           // of one chunk's record
-    size_t rec, segE, tr, S, dS, u, du, trT, dseg, total;
+    size_t rec, segE, tr, S, dS, u, du, trT, dseg, acc, total;
 };
 
 // Validates sizes, types and strides, not pointers.  step: of pgf_gdr_step.
