@@ -449,11 +449,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 Frag<PO> so;
 #pragma unroll
                 for (int p = 0; p < PO; ++p) so.p[p] = sp.p[p];
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    kS[m] = mfma_parts<P, 3>(kf[ks & 1][m], sp, kS[m]);
-                    if constexpr (OUT) qS[m] = mfma_parts<P, PO>(qf[ks & 1][m], so, qS[m]);
-                }
+                mfma_parts2<P, 3>(kf[ks & 1], sp, kS);
+                if constexpr (OUT) mfma_parts2<P, PO>(qf[ks & 1], so, qS);
                 __builtin_amdgcn_sched_barrier(0);
             }
             floatx4 X[2];
@@ -482,9 +479,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             read_kt(0);
             const float end = s.eG[31];
             __builtin_amdgcn_sched_barrier(0);
-            floatx4 W[2];
-#pragma unroll
-            for (int m = 0; m < 2; ++m) W[m] = mfma_parts<3, 3>(tf[m], xp, floatx4{0.0f, 0.0f, 0.0f, 0.0f});
+            floatx4 W[2] = {};
+            mfma_parts2<3, 3>(tf, xp, W);
             const Frag<3> wp = to_frag<3>(W[0], W[1]);
             Frag<MODE == kOut ? PO : 3> af[2];
             if constexpr (MODE != kSegment) {
@@ -518,22 +514,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
                 for (int p = 0; p < PO; ++p) xo.p[p] = xp.p[p];
                 const Buf ob = make_buf(op + (int64_t)ch * kC * a.o.st, ost, live_rows(ch), a.dv * (int)sizeof(T));
+                mfma_parts2<PO, PO>(af, xo, qS);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const floatx4 o = mfma_parts<PO, PO>(af[m], xo, qS[m]);
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * m + j) * ost, o[j] * a.scale);
-                }
+                    for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * m + j) * ost, qS[m][j] * a.scale);
             }
             if constexpr (MODE == kSave) {
                 float *eb = a.saveE + ((slot0 + ch) * a.Hv + h) * (int64_t)(kC * a.dv);
+                floatx4 e[2] = {};
+                mfma_parts2<3, 3>(af, xp, e);
+                if (live_col) {
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const floatx4 e = mfma_parts<3, 3>(af[m], xp, floatx4{0.0f, 0.0f, 0.0f, 0.0f});
-                    if (live_col) {
+                    for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) *at_off(eb, (uint32_t)((16 * m + 4 * qd + j) * a.dv + col) * 4u) = e[j];
-                    }
+                        for (int j = 0; j < 4; ++j) *at_off(eb, (uint32_t)((16 * m + 4 * qd + j) * a.dv + col) * 4u) = e[m][j];
                 }
             }
         }

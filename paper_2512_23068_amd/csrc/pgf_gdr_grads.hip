@@ -207,12 +207,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (ks == 0) {
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) dE[m] = mfma_parts<3, P>(af[m], gf, floatx4{0.0f, 0.0f, 0.0f, 0.0f});
+                    dE[0] = dE[1] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                    mfma_parts2<3, P>(af, gf, dE);
                 }
                 const Frag<3> sp = to_frag<3>(S[2 * ks], S[2 * ks + 1]);
-#pragma unroll
-                for (int m = 0; m < 2; ++m) x[m] = mfma_parts<P, 3>(kf[ks & 1][m], sp, x[m]);
+                mfma_parts2<P, 3>(kf[ks & 1], sp, x);
                 __builtin_amdgcn_sched_barrier(0);
             }
             const Frag<3> xp = to_frag<3>(x[0], x[1]);
@@ -244,10 +243,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                     dE[m][j] *= a.scale;
                     gs[m][j] = a.scale * eG[m][j] * g[m][j];
                 }
-                dE[m] = mfma_parts<3, 3>(tf[m], xp, dE[m]);
+            }
+            mfma_parts2<3, 3>(tf, xp, dE);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) es[m][j] = -eG[m][j] * dE[m][j];
-            }
             const Frag<3> gp3 = to_frag<3>(gs[0], gs[1]), ep3 = to_frag<3>(es[0], es[1]);
 #pragma unroll
             for (int gr = 0; gr < KT / GK; ++gr) {
