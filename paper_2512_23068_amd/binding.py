@@ -11,6 +11,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -137,7 +138,7 @@ def lib():
     L.pgf_la_plan.argtypes = [LP, ctypes.POINTER(PgfPlanInfo)]
     L.pgf_la_scan_jvp.restype = ctypes.c_int
     L.pgf_la_scan_jvp.argtypes = [ctypes.c_void_p] * 8 + [LP, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]
-    GP, QP, V = ctypes.POINTER(PgfGdrParams), ctypes.POINTER(PgfQkParams), ctypes.c_void_p
+    V = GP = QP = ctypes.c_void_p      # (parameter blocks as bytes)
     L.pgf_gdr_workspace_bytes.restype = ctypes.c_size_t
     L.pgf_gdr_workspace_bytes.argtypes = [GP]
     L.pgf_gdr_plan.restype = ctypes.c_int
@@ -610,110 +611,147 @@ def _la_scan_jvp_on(ts, S_in, dS_in, return_state, seg_len, chunk_segs, workspac
     return (o, do) + states
 
 
-def _rows(t, shape, dev, name, dtypes):
-    """An input [B, H, L, ..] as the kernels read it: on dev, of one of dtypes,
-    its last index dense and its address and strides in units of 16 bytes (of
-    the element for [B, H, L]); anything else is copied."""
-    if not (isinstance(t, torch.Tensor) and t.device == dev and t.dtype in dtypes):
-        raise ValueError(f"{name}: expected a {' or '.join(str(d) for d in dtypes)} tensor on {dev}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    moves = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
-    return t if _in_place(t) and (any(moves) or not moves) else t.clone(memory_format=torch.contiguous_format)
+def _bad(t, shape, dev, dtype, name):
+    if not (isinstance(t, torch.Tensor) and t.device == dev and t.dtype == dtype):
+        raise ValueError(f"{name}: expected a {dtype} tensor on {dev}")
+    raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _in_place(t):
-    """Whether the kernels can take t's rows where they are."""
-    if t.numel() == 0 or t.dim() == 3:
-        return True
-    unit = 16 // t.element_size()
-    st = [s for s, n in zip(t.stride()[:3], t.shape[:3]) if n > 1]
-    return (t.stride(3) == 1 or t.shape[3] == 1) and t.data_ptr() % 16 == 0 and all(s % unit == 0 for s in st)
+def _rows(t, shape, dev, dtype, name):
+    """An input [B, H, L(, d)] as the kernels read it, and its strides {batch,
+    head, step} (zero where the index does not move).  A tensor whose last index
+    is not dense, whose address or strides are not multiples of 16 bytes, or
+    that is one row for all indexes (strides of zero throughout mean dense rows)
+    is copied."""
+    if t.dtype is not dtype or t.shape != shape or t.device != dev:
+        _bad(t, shape, dev, dtype, name)
+    B, H, L = shape[:3]
+    st = t.stride()
+    sb, sh, sl = st[0] if B > 1 else 0, st[1] if H > 1 else 0, st[2] if L > 1 else 0
+    if len(shape) == 4:
+        unit = 8 if dtype is torch.bfloat16 else 4
+        ok = (st[3] == 1 or shape[3] == 1) and not ((sb | sh | sl) % unit or t.data_ptr() % 16)
+    else:
+        ok = True
+    if not ((ok and (sb or sh or sl or B * H * L <= 1)) or t.numel() == 0):
+        return _rows(t.clone(memory_format=torch.contiguous_format), shape, dev, dtype, name)
+    return t, (sb, sh, sl)
 
 
-def _set_strides(field, t):
-    """Strides of [B, H, L, ..] (of indexes that move)."""
-    field[0], field[1], field[2] = (0 if n <= 1 else s for s, n in zip(t.stride()[:3], t.shape[:3]))
+def _new_rows(t, strides, dtype=None):
+    """A new output in the shape and order of t: step-major where t's heads lie
+    side by side in each step.  Returns it with its strides."""
+    B, H, L, d = t.shape
+    if H > 1 and L > 1 and strides[1] < strides[2]:
+        return (torch.empty((B, L, H, d), device=t.device, dtype=t.dtype).transpose(1, 2), (L * H * d, d, H * d))
+    return torch.empty((B, H, L, d), device=t.device, dtype=t.dtype), (H * L * d, L * d, d)
 
 
-def _like_rows(t, shape, dtype):
-    """A new output [B, H, L, d] in the order of t: step-major where t's heads
-    lie side by side in each step."""
-    B, H, L, d = shape
-    if t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) < t.stride(2):
-        return torch.empty((B, L, H, d), device=t.device, dtype=dtype).transpose(1, 2)
-    return torch.empty(shape, device=t.device, dtype=dtype)
-
-
-def _check_rows_out(t, shape, dtype, dev, name):
-    """A caller's output [B, H, L, d] with any strides the kernels can write."""
-    if not (isinstance(t, torch.Tensor) and t.dtype == dtype and t.device == dev and tuple(t.shape) == tuple(shape)
-            and _in_place(t) and all(s > 0 for s, n in zip(t.stride(), t.shape) if n > 1)):
-        raise ValueError(f"{name}: expected a {dtype} tensor of shape {tuple(shape)} on {dev} with dense rows of "
-                         "16-byte aligned address and strides")
-    return t
+def _rows_out(t, like, name):
+    """A caller's output of the shape, type and device of `like`, with any strides
+    the kernels can write.  Returns it with its strides."""
+    ok = (isinstance(t, torch.Tensor) and t.dtype == like.dtype and t.device == like.device and t.shape == like.shape)
+    if ok and t.numel():
+        unit = 16 // t.element_size()
+        st = [s if n > 1 else 0 for s, n in zip(t.stride(), t.shape)]
+        ok = ((t.stride(3) == 1 or t.shape[3] == 1) and t.data_ptr() % 16 == 0
+              and all(s % unit == 0 and s > 0 for s, n in zip(st[:3], t.shape) if n > 1))
+    if not ok:
+        raise ValueError(f"{name}: expected a {like.dtype} tensor of shape {tuple(like.shape)} on {like.device} with "
+                         "dense rows of 16-byte aligned address and strides")
+    return t, tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:3], t.shape))
 
 
 def _state(t, shape, dev, name):
-    """A state the kernels read or write in place (float32, dense)."""
+    """Address of a state the kernels read or write in place (float32, dense), or None."""
     if t is None:
-        return None
-    if not (isinstance(t, torch.Tensor) and t.dtype == torch.float32 and t.device == dev
-            and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.data_ptr() % 16 == 0):
+        return 0
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.device == dev
+            and t.shape == shape and t.is_contiguous() and t.data_ptr() % 16 == 0):
         raise ValueError(f"{name}: expected a contiguous float32 tensor of shape {tuple(shape)} on {dev}")
-    return t
+    return t.data_ptr()
 
 
-def _gdr_inputs(q, k, v, g, beta, scale, seg_len):
-    """Checks shapes and fills the common fields; returns (params, tensors)."""
-    if q.dim() != 4 or v.dim() != 4 or k.shape != q.shape:
-        raise ValueError("shapes: q, k [B,Hk,L,dk], v [B,Hv,L,dv], g, beta [B,Hv,L]")
-    if q.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("q, k and v must all be float32 or all bfloat16")
-    dev, dt = q.device, (q.dtype,)
-    B, Hk, L, dk = q.shape
-    Hv, dv = v.shape[1], v.shape[3]
-    q, k = _rows(q, (B, Hk, L, dk), dev, "q", dt), _rows(k, (B, Hk, L, dk), dev, "k", dt)
-    v = _rows(v, (B, Hv, L, dv), dev, "v", dt)
-    g = _rows(g, (B, Hv, L), dev, "g", (torch.float32,))
-    beta = _rows(beta, (B, Hv, L), dev, "beta", (torch.float32,))
-    p = PgfGdrParams()
-    p.batch, p.key_heads, p.value_heads, p.seqlen, p.d_key, p.d_value = B, Hk, Hv, L, dk, dv
-    p.in_dtype = PGF_BF16 if q.dtype == torch.bfloat16 else PGF_F32
-    p.seg_len = int(seg_len)
-    p.scale = float(dk ** -0.5 if scale is None else scale)
-    for field, t in ((p.q_strides, q), (p.k_strides, k), (p.v_strides, v), (p.g_strides, g),
-                     (p.beta_strides, beta)):
-        _set_strides(field, t)
-    return p, (q, k, v, g, beta)
+# The parameter structs as struct.pack lays them out (native alignment): one
+# call fills all fields, where a ctypes structure takes one per field; a call's
+# host time is what a single token waits for.
+_GDR_PACK = struct.Struct("@7qPiifi27q5PqPPN")
+_QK_PACK = struct.Struct("@6qiiif18q4PiqPPPN")
+_NO = (0, 0, 0)
 
 
-def _gdr_packed(p, cu_seqlens, B, dev):
-    """Sets the packed sequences; returns the number of sequences."""
-    if cu_seqlens is None:
-        return B
-    c = cu_seqlens
-    if not (isinstance(c, torch.Tensor) and c.device == dev and c.dtype == torch.int32 and c.dim() == 1
-            and c.numel() >= 2 and c.is_contiguous()):
-        raise ValueError(f"cu_seqlens: expected a contiguous int32 tensor [sequences + 1] on {dev}")
-    if B != 1:
-        raise ValueError("cu_seqlens: packed sequences take a batch of 1")
-    p.n_seqs, p.cu_seqlens = c.numel() - 1, c.data_ptr()
-    return c.numel() - 1
+def _on(dev, stream):
+    """Context of a call: the tensors' device and the caller's stream, where they
+    are not current already."""
+    if stream is None and dev.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    stack = contextlib.ExitStack()
+    stack.enter_context(torch.cuda.device(dev))
+    stack.enter_context(_on_stream(stream, dev))
+    return stack
 
 
-def _gdr_workspace(L_, p, workspace, dev):
-    nbytes = int(L_.pgf_gdr_workspace_bytes(ctypes.byref(p)))
-    if nbytes == 0:
-        _check(L_.pgf_gdr_plan(ctypes.byref(p), ctypes.byref(ctypes.c_int32())))
-    workspace = _checked_workspace(workspace, nbytes, dev)
-    p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    return workspace
+def _stream_of(dev):
+    return torch.cuda.current_stream(dev).cuda_stream
 
 
-def _all_on_device(*ts):
-    if not all(isinstance(t, torch.Tensor) and t.is_cuda for t in ts):
-        raise ValueError("q, k, v, g and beta must be device tensors")
+def _on_device(names, *ts):
+    for t in ts:
+        if not (isinstance(t, torch.Tensor) and t.is_cuda):
+            raise ValueError(f"{names} must be device tensors")
+
+
+class _Gdr:
+    """Checked arguments of a call of the gated delta rule."""
+
+    def __init__(self, q, k, v, g, beta, scale, seg_len):
+        if q.dim() != 4 or v.dim() != 4:
+            raise ValueError("shapes: q, k [B,Hk,L,dk], v [B,Hv,L,dv], g, beta [B,Hv,L]")
+        dt, dev = q.dtype, q.device
+        if dt is not torch.float32 and dt is not torch.bfloat16:
+            raise ValueError("q, k and v must all be float32 or all bfloat16")
+        self.dev, self.dt = dev, dt
+        B, Hk, L, dk = qs = q.shape
+        Hv, dv = v.shape[1], v.shape[3]
+        gs = (B, Hv, L)
+        self.q, s0 = _rows(q, qs, dev, dt, "q")
+        self.k, s1 = _rows(k, qs, dev, dt, "k")
+        self.v, self.vs = _rows(v, (B, Hv, L, dv), dev, dt, "v")
+        self.g, s3 = _rows(g, gs, dev, torch.float32, "g")
+        self.beta, s4 = _rows(beta, gs, dev, torch.float32, "beta")
+        self.qs, self.ks = s0, s1
+        self.strides = s0 + s1 + self.vs + s3 + s4
+        self.sizes = (B, Hk, Hv, L, dk, dv)
+        self.B, self.cell = B, (B, Hv, dk, dv)
+        self.scale = float(dk ** -0.5 if scale is None else scale)
+        self.seg_len = int(seg_len)
+        self.n_seqs = self.cu = 0
+
+    def packed(self, c):
+        if c is None:
+            return
+        if not (isinstance(c, torch.Tensor) and c.device == self.dev and c.dtype == torch.int32 and c.dim() == 1
+                and c.numel() >= 2 and c.is_contiguous()):
+            raise ValueError(f"cu_seqlens: expected a contiguous int32 tensor [sequences + 1] on {self.dev}")
+        if self.B != 1:
+            raise ValueError("cu_seqlens: packed sequences take a batch of 1")
+        self.n_seqs, self.cu = c.numel() - 1, c.data_ptr()
+        self.cell = (self.n_seqs,) + self.cell[1:]
+
+    def pack(self, o, grads=0, out=_NO * 3, states=(0, 0, 0, 0), pool=(0, 0, 0), workspace=None):
+        ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
+        return _GDR_PACK.pack(*self.sizes, self.n_seqs, self.cu, self.dt is torch.bfloat16, self.seg_len, self.scale,
+                              grads, *self.strides, *o, *out, *states, *pool, *ws)
+
+    def workspace(self, given, grads=0):
+        p = self.pack(_NO, grads)
+        nbytes = lib().pgf_gdr_workspace_bytes(p)
+        if nbytes == 0:
+            _check(lib().pgf_gdr_plan(p, ctypes.byref(ctypes.c_int32())))
+        return _checked_workspace(given, nbytes, self.dev)
+
+    def inputs(self):
+        return self.q.data_ptr(), self.k.data_ptr(), self.v.data_ptr(), self.g.data_ptr(), self.beta.data_ptr()
 
 
 def gdr_scan(q, k, v, g, beta, *, scale=None, S_in=None, return_state=False, cu_seqlens=None, qk_prep=None, seg_len=0,
@@ -731,33 +769,23 @@ def gdr_scan(q, k, v, g, beta, *, scale=None, S_in=None, return_state=False, cu_
     arguments of qk_norm, which then prepares q and k first.
     Returns o [B,Hv,L,dv] in q's type, with return_state (o, S_out).
     """
-    _all_on_device(q, k, v, g, beta)
-    with torch.cuda.device(q.device), _on_stream(stream, q.device):
-        L_ = lib()
+    _on_device("q, k, v, g and beta", q, k, v, g, beta)
+    with _on(q.device, stream):
         if qk_prep is not None:
             q, k = qk_norm(q, k, **qk_prep)
-        p, (q, k, v, g, beta) = _gdr_inputs(q, k, v, g, beta, scale, seg_len)
-        dev = q.device
-        B, Hv, L, dv = v.shape
-        n = _gdr_packed(p, cu_seqlens, B, dev)
-        cell = (n, Hv, q.shape[3], dv)
-        S_in = _state(S_in, cell, dev, "S_in")
-        p.S_in = None if S_in is None else S_in.data_ptr()
+        c = _Gdr(q, k, v, g, beta, scale, seg_len)
+        c.packed(cu_seqlens)
+        S0 = _state(S_in, c.cell, c.dev, "S_in")
         if out is None:
-            o = _like_rows(v, v.shape, q.dtype)
+            o, os = _new_rows(c.v, c.vs)
             if cu_seqlens is not None:
                 o.zero_()
         else:
-            o = _check_rows_out(out, v.shape, q.dtype, dev, "out")
-        _set_strides(p.o_strides, o)
-        workspace = _gdr_workspace(L_, p, workspace, dev)
-        S_out = None
-        if return_state:
-            S_out = torch.empty(cell, device=dev, dtype=torch.float32)
-            p.S_out = S_out.data_ptr()
-        st = torch.cuda.current_stream(dev).cuda_stream
-        _check(L_.pgf_gdr_scan(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), ctypes.byref(p), _ptr(o),
-                               ctypes.c_void_p(st)))
+            o, os = _rows_out(out, c.v, "out")
+        workspace = c.workspace(workspace)
+        S_out = torch.empty(c.cell, device=c.dev, dtype=torch.float32) if return_state else None
+        p = c.pack(os, states=(S0, S_out.data_ptr() if return_state else 0, 0, 0), workspace=workspace)
+        _check(lib().pgf_gdr_scan(*c.inputs(), p, o.data_ptr(), _stream_of(c.dev)))
         return (o, S_out) if return_state else o
 
 
@@ -767,47 +795,36 @@ def gdr_grads(q, k, v, g, beta, do, *, scale=None, S_in=None, dS_out=None, cu_se
     do = dl/do [B,Hv,L,dv] (in q's type) and dS_out = dl/dS_out (float32, None:
     zero).
 
-    Inputs as in gdr_scan (of q and k after their preparation).  out: optional
+    Inputs as in gdr_scan (q and k after their preparation).  out: optional
     (dq, dk, dv) outputs.  Returns (dq, dk, dv) in q's type, dg and dbeta
     [B,Hv,L] float32, and with S_in or dS_out also dS_in (float32).  Gradients of
     rows of no packed sequence are zero where the output is a new one.
     """
-    _all_on_device(q, k, v, g, beta)
-    with torch.cuda.device(q.device), _on_stream(stream, q.device):
-        L_ = lib()
-        p, (q, k, v, g, beta) = _gdr_inputs(q, k, v, g, beta, scale, seg_len)
-        p.grads = 1
-        dev = q.device
-        B, Hv, L, dv = v.shape
-        do = _rows(do, v.shape, dev, "do", (q.dtype,))
-        _set_strides(p.o_strides, do)
-        n = _gdr_packed(p, cu_seqlens, B, dev)
-        cell = (n, Hv, q.shape[3], dv)
-        S_in, dS_out = _state(S_in, cell, dev, "S_in"), _state(dS_out, cell, dev, "dS_out")
-        p.S_in = None if S_in is None else S_in.data_ptr()
-        p.dS_out = None if dS_out is None else dS_out.data_ptr()
+    _on_device("q, k, v, g, beta and do", q, k, v, g, beta, do)
+    with _on(q.device, stream):
+        c = _Gdr(q, k, v, g, beta, scale, seg_len)
+        do, ds = _rows(do, c.v.shape, c.dev, c.dt, "do")
+        c.packed(cu_seqlens)
+        S0, dS1 = _state(S_in, c.cell, c.dev, "S_in"), _state(dS_out, c.cell, c.dev, "dS_out")
         if out is None:
-            grads = [_like_rows(t, t.shape, q.dtype) for t in (q, k, v)]
-            if cu_seqlens is not None:
-                for t in grads:
-                    t.zero_()
+            grads = [_new_rows(t, st) for t, st in ((c.q, c.qs), (c.k, c.ks), (c.v, c.vs))]
         else:
             if len(out) != 3:
                 raise ValueError("out: expected (dq, dk, dv)")
-            grads = [_check_rows_out(o, t.shape, q.dtype, dev, f"out[{i}]") for i, (o, t) in enumerate(zip(out, (q, k, v)))]
-        for field, t in zip((p.dq_strides, p.dk_strides, p.dv_strides), grads):
-            _set_strides(field, t)
-        new = torch.empty if cu_seqlens is None else torch.zeros
-        dg, dbeta = (new((B, Hv, L), device=dev, dtype=torch.float32) for _ in range(2))
+            grads = [_rows_out(t, like, f"out[{i}]") for i, (t, like) in enumerate(zip(out, (c.q, c.k, c.v)))]
+        dg, dbeta = (torch.empty(c.g.shape, device=c.dev, dtype=torch.float32) for _ in range(2))
+        if cu_seqlens is not None:
+            for t in ([t for t, _ in grads] if out is None else []) + [dg, dbeta]:
+                t.zero_()
         dS_in = None
         if S_in is not None or dS_out is not None:
-            dS_in = torch.empty(cell, device=dev, dtype=torch.float32)
-            p.dS_in = dS_in.data_ptr()
-        workspace = _gdr_workspace(L_, p, workspace, dev)
-        st = torch.cuda.current_stream(dev).cuda_stream
-        _check(L_.pgf_gdr_grads(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(do), ctypes.byref(p),
-                                *[_ptr(t) for t in grads], _ptr(dg), _ptr(dbeta), ctypes.c_void_p(st)))
-        return (*grads, dg, dbeta) + (() if dS_in is None else (dS_in,))
+            dS_in = torch.empty(c.cell, device=c.dev, dtype=torch.float32)
+        workspace = c.workspace(workspace, 1)
+        p = c.pack(ds, 1, grads[0][1] + grads[1][1] + grads[2][1],
+                   (S0, 0, dS1, 0 if dS_in is None else dS_in.data_ptr()), workspace=workspace)
+        _check(lib().pgf_gdr_grads(*c.inputs(), do.data_ptr(), p, *[t.data_ptr() for t, _ in grads], dg.data_ptr(),
+                                   dbeta.data_ptr(), _stream_of(c.dev)))
+        return tuple(t for t, _ in grads) + (dg, dbeta) + (() if dS_in is None else (dS_in,))
 
 
 def gdr_step(q, k, v, g, beta, S, *, slots=None, scale=None, qk_prep=None, out=None, stream=None):
@@ -819,80 +836,73 @@ def gdr_step(q, k, v, g, beta, S, *, slots=None, scale=None, qk_prep=None, out=N
     An entry whose slot is not a state of the pool (-1: padding), or is that of
     an earlier entry, has zero outputs and changes nothing.  Returns o.
     """
-    _all_on_device(q, k, v, g, beta)
-    with torch.cuda.device(q.device), _on_stream(stream, q.device):
-        L_ = lib()
+    _on_device("q, k, v, g, beta and S", q, k, v, g, beta, S)
+    with _on(q.device, stream):
         if qk_prep is not None:
             q, k = qk_norm(q, k, **qk_prep)
-        p, (q, k, v, g, beta) = _gdr_inputs(q, k, v, g, beta, scale, 0)
-        dev = q.device
-        B, Hv, L, dv = v.shape
-        if not isinstance(S, torch.Tensor) or S.dim() != 4:
+        c = _Gdr(q, k, v, g, beta, scale, 0)
+        if S.dim() != 4:
             raise ValueError("S: expected states [pool,Hv,dk,dv]")
-        _state(S, (S.shape[0], Hv, q.shape[3], dv), dev, "S")
-        p.S_pool, p.pool = S.data_ptr(), S.shape[0]
+        pool = S.shape[0]
+        ptr, at = _state(S, (pool,) + c.cell[1:], c.dev, "S"), 0
         if slots is not None:
-            if not (isinstance(slots, torch.Tensor) and slots.device == dev and slots.dtype == torch.int32
-                    and tuple(slots.shape) == (B,) and slots.is_contiguous()):
-                raise ValueError(f"slots: expected a contiguous int32 tensor [{B}] on {dev}")
-            p.slots = slots.data_ptr()
-        elif S.shape[0] < B:
-            raise ValueError(f"S: {S.shape[0]} states for {B} entries")
-        o = _like_rows(v, v.shape, q.dtype) if out is None else _check_rows_out(out, v.shape, q.dtype, dev, "out")
-        _set_strides(p.o_strides, o)
-        st = torch.cuda.current_stream(dev).cuda_stream
-        _check(L_.pgf_gdr_step(_ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), ctypes.byref(p), _ptr(o),
-                               ctypes.c_void_p(st)))
+            if not (isinstance(slots, torch.Tensor) and slots.device == c.dev and slots.dtype is torch.int32
+                    and slots.shape == (c.B,) and slots.is_contiguous()):
+                raise ValueError(f"slots: expected a contiguous int32 tensor [{c.B}] on {c.dev}")
+            at = slots.data_ptr()
+        elif pool < c.B:
+            raise ValueError(f"S: {pool} states for {c.B} entries")
+        o, os = _new_rows(c.v, c.vs) if out is None else _rows_out(out, c.v, "out")
+        p = c.pack(os, pool=(ptr, pool, at))
+        _check(lib().pgf_gdr_step(*c.inputs(), p, o.data_ptr(), _stream_of(c.dev)))
         return o
 
 
-def _qk_params(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved, keep):
-    """Checks the arguments shared by qk_norm and its adjoint."""
-    if q.dim() != 4 or k.dim() != 4 or (k.shape[0], k.shape[2], k.shape[3]) != (q.shape[0], q.shape[2], q.shape[3]):
-        raise ValueError("shapes: q [B,Hq,L,d], k [B,Hk,L,d]")
-    if q.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError("q and k must both be float32 or both bfloat16")
-    if norm not in NORMS:
-        raise ValueError(f"norm: one of {', '.join(NORMS)}")
-    dev = q.device
-    B, Hq, L, d = q.shape
-    q, k = _rows(q, q.shape, dev, "q", (q.dtype,)), _rows(k, k.shape, dev, "k", (q.dtype,))
-    p = PgfQkParams()
-    p.batch, p.q_heads, p.k_heads, p.seqlen, p.d_head = B, Hq, k.shape[1], L, d
-    p.in_dtype = PGF_BF16 if q.dtype == torch.bfloat16 else PGF_F32
-    p.norm, p.eps, p.interleaved = NORMS[norm], float(eps), int(bool(interleaved))
-    wq, wk = _dev_param(wq, (d,), dev, "wq"), _dev_param(wk, (d,), dev, "wk")
-    p.w_q, p.w_k = (None if w is None else w.data_ptr() for w in (wq, wk))
-    if inv_freq is not None:
-        if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
-            raise ValueError("inv_freq: expected a tensor [rot / 2]")
-        inv_freq = _dev_param(inv_freq, inv_freq.shape, dev, "inv_freq")
-        p.rot, p.inv_freq = 2 * inv_freq.numel(), inv_freq.data_ptr()
-        if positions is not None:
-            if not (isinstance(positions, torch.Tensor) and positions.device == dev
-                    and positions.dtype in (torch.int32, torch.int64)
-                    and tuple(positions.shape) in ((L,), (1, L), (B, L))):
-                raise ValueError(f"positions: expected int32 or int64 [{L}] or [{B},{L}] on {dev}")
-            if L > 1 and positions.stride(-1) != 1:
-                positions = positions.contiguous()
-            p.positions, p.pos_bits = positions.data_ptr(), 8 * positions.element_size()
-            p.pos_stride = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
-    _set_strides(p.q_strides, q)
-    _set_strides(p.k_strides, k)
-    keep += [wq, wk, inv_freq, positions]
-    return p, q, k
+class _Qk:
+    """Checked arguments of a call of the query/key preparation."""
 
+    def __init__(self, q, k, wq, wk, norm, eps, positions, inv_freq, interleaved):
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("shapes: q [B,Hq,L,d], k [B,Hk,L,d]")
+        dt, dev = q.dtype, q.device
+        if dt is not torch.float32 and dt is not torch.bfloat16:
+            raise ValueError("q and k must both be float32 or both bfloat16")
+        if norm not in NORMS:
+            raise ValueError(f"norm: one of {', '.join(NORMS)}")
+        B, Hq, L, d = q.shape
+        Hk = k.shape[1]
+        self.dev, self.d = dev, d
+        self.q, self.qs = _rows(q, q.shape, dev, dt, "q")
+        self.k, self.ks = _rows(k, (B, Hk, L, d), dev, dt, "k")
+        self.wq, self.wk = _dev_param(wq, (d,), dev, "wq"), _dev_param(wk, (d,), dev, "wk")
+        rot = pos = stride = bits = 0
+        if inv_freq is not None:
+            if not isinstance(inv_freq, torch.Tensor) or inv_freq.dim() != 1:
+                raise ValueError("inv_freq: expected a tensor [rot / 2]")
+            inv_freq = _dev_param(inv_freq, inv_freq.shape, dev, "inv_freq")
+            rot = 2 * inv_freq.numel()
+            if rot and positions is not None:
+                if not (isinstance(positions, torch.Tensor) and positions.device == dev
+                        and positions.dtype in (torch.int32, torch.int64)
+                        and tuple(positions.shape) in ((L,), (1, L), (B, L))):
+                    raise ValueError(f"positions: expected int32 or int64 [{L}] or [{B},{L}] on {dev}")
+                if L > 1 and positions.stride(-1) != 1:
+                    positions = positions.contiguous()
+                pos, bits = positions.data_ptr(), 8 * positions.element_size()
+                stride = positions.stride(0) if positions.dim() == 2 and positions.shape[0] > 1 else 0
+        self.keep = (inv_freq, positions)
+        ptr = [0 if t is None else t.data_ptr() for t in (self.wq, self.wk, inv_freq)]
+        self.head = (B, Hq, Hk, L, d, rot, dt is torch.bfloat16, NORMS[norm], bool(interleaved), float(eps))
+        self.tail = (*ptr, pos, bits, stride)
 
-def _qk_outputs(p, q, k, out, names):
-    if out is None:
-        qo, ko = _like_rows(q, q.shape, q.dtype), _like_rows(k, k.shape, k.dtype)
-    else:
+    def outputs(self, out):
+        if out is None:
+            return _new_rows(self.q, self.qs) + _new_rows(self.k, self.ks)
         qo, ko = out
-        _check_rows_out(qo, q.shape, q.dtype, q.device, names[0])
-        _check_rows_out(ko, k.shape, k.dtype, q.device, names[1])
-    _set_strides(p.q_out_strides, qo)
-    _set_strides(p.k_out_strides, ko)
-    return qo, ko
+        return _rows_out(qo, self.q, "out[0]") + _rows_out(ko, self.k, "out[1]")
+
+    def pack(self, qos, kos, dqs=_NO, dks=_NO, gw=(0, 0), ws=(0, 0)):
+        return _QK_PACK.pack(*self.head, *self.qs, *self.ks, *qos, *kos, *dqs, *dks, *self.tail, *gw, *ws)
 
 
 def qk_norm(q, k, *, wq=None, wk=None, norm="rms", eps=1e-6, positions=None, inv_freq=None, interleaved=False,
@@ -907,14 +917,12 @@ def qk_norm(q, k, *, wq=None, wk=None, norm="rms", eps=1e-6, positions=None, inv
     out: optional (q, k) outputs, which may be the inputs themselves.
     Returns (q, k) prepared, in the inputs' type and order.
     """
-    if not (isinstance(q, torch.Tensor) and isinstance(k, torch.Tensor) and q.is_cuda and k.is_cuda):
-        raise ValueError("q and k must be device tensors")
-    with torch.cuda.device(q.device), _on_stream(stream, q.device):
-        L_, keep = lib(), []
-        p, q, k = _qk_params(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved, keep)
-        qo, ko = _qk_outputs(p, q, k, out, ("out[0]", "out[1]"))
-        st = torch.cuda.current_stream(q.device).cuda_stream
-        _check(L_.pgf_qk_norm(_ptr(q), _ptr(k), ctypes.byref(p), _ptr(qo), _ptr(ko), ctypes.c_void_p(st)))
+    _on_device("q and k", q, k)
+    with _on(q.device, stream):
+        c = _Qk(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved)
+        qo, qos, ko, kos = c.outputs(out)
+        _check(lib().pgf_qk_norm(c.q.data_ptr(), c.k.data_ptr(), c.pack(qos, kos), qo.data_ptr(), ko.data_ptr(),
+                                 _stream_of(c.dev)))
         return qo, ko
 
 
@@ -925,26 +933,20 @@ def qk_norm_grads(q, k, dq, dk, *, wq=None, wk=None, norm="rms", eps=1e-6, posit
     Returns dl/dq and dl/dk in the inputs' type, then dl/dwq and dl/dwk [d]
     float32 for the weights that are given.
     """
-    if not all(isinstance(t, torch.Tensor) and t.is_cuda for t in (q, k, dq, dk)):
-        raise ValueError("q, k, dq and dk must be device tensors")
-    with torch.cuda.device(q.device), _on_stream(stream, q.device):
-        L_, keep = lib(), []
-        p, q, k = _qk_params(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved, keep)
-        dq, dk = _rows(dq, q.shape, q.device, "dq", (q.dtype,)), _rows(dk, k.shape, q.device, "dk", (q.dtype,))
-        _set_strides(p.dq_strides, dq)
-        _set_strides(p.dk_strides, dk)
-        qo, ko = _qk_outputs(p, q, k, out, ("out[0]", "out[1]"))
-        gw = []
-        for w, field in ((wq, "grad_w_q"), (wk, "grad_w_k")):
-            if w is not None:
-                gw.append(torch.empty(q.shape[3], device=q.device, dtype=torch.float32))
-                setattr(p, field, gw[-1].data_ptr())
-        workspace = _checked_workspace(workspace, int(L_.pgf_qk_norm_workspace_bytes(ctypes.byref(p))), q.device)
-        p.workspace, p.workspace_bytes = workspace.data_ptr(), workspace.numel()
-        st = torch.cuda.current_stream(q.device).cuda_stream
-        _check(L_.pgf_qk_norm_grads(_ptr(q), _ptr(k), _ptr(dq), _ptr(dk), ctypes.byref(p), _ptr(qo), _ptr(ko),
-                                    ctypes.c_void_p(st)))
-        return (qo, ko, *gw)
+    _on_device("q, k, dq and dk", q, k, dq, dk)
+    with _on(q.device, stream):
+        c = _Qk(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved)
+        dq, dqs = _rows(dq, c.q.shape, c.dev, c.q.dtype, "dq")
+        dk, dks = _rows(dk, c.k.shape, c.dev, c.q.dtype, "dk")
+        qo, qos, ko, kos = c.outputs(out)
+        gw = [None if w is None else torch.empty(c.d, device=c.dev, dtype=torch.float32) for w in (wq, wk)]
+        nbytes = lib().pgf_qk_norm_workspace_bytes(c.pack(qos, kos, dqs, dks))
+        workspace = _checked_workspace(workspace, nbytes, c.dev)
+        p = c.pack(qos, kos, dqs, dks, tuple(0 if t is None else t.data_ptr() for t in gw),
+                   (workspace.data_ptr(), workspace.numel()))
+        _check(lib().pgf_qk_norm_grads(c.q.data_ptr(), c.k.data_ptr(), dq.data_ptr(), dk.data_ptr(), p, qo.data_ptr(),
+                                       ko.data_ptr(), _stream_of(c.dev)))
+        return (qo, ko, *[t for t in gw if t is not None])
 
 
 def timing_enable(on: bool = True):

@@ -23,7 +23,7 @@ bool strides_ok(const int64_t (&s)[3], int64_t unit, bool out, int64_t B, int64_
     const bool dense = !s[0] && !s[1] && !s[2];
     for (int i = 0; i < 3; ++i) {
         if (s[i] < 0 || s[i] > kMaxStride || s[i] % unit) return false;
-        if (out && !dense && n[i] > 1 && !s[i]) return false;
+        if (out && !dense && L > 0 && n[i] > 1 && !s[i]) return false;
     }
     return true;
 }
