@@ -176,7 +176,7 @@ int make_plan(const pgf_qk_params *p, Plan *out, bool grads) {
     while (q.G * 8 < q.d) q.G *= 2;
     // Blocks of the gradient kernel: enough to fill the GPU several times; each
     // leaves one partial sum of the weights' gradients.
-    q.blocks = std::min<int64_t>(std::max<int64_t>(1, q.B * q.L), 2048);
+    q.blocks = std::min<int64_t>(std::max<int64_t>(1, q.B * q.L), 1024);
     q.total = grads && (p->w_q || p->w_k) ? (size_t)q.blocks * 2 * q.d * sizeof(float) : 0;
     *out = q;
     return PGF_OK;

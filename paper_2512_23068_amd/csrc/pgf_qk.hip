@@ -6,11 +6,13 @@
 // and, t = du * w,  dx = r (t - c r^2 x (x . t)).
 //
 // One pass: a group of G = 2^n >= d / 8 lanes holds one head vector, eight
-// elements a lane (16 bytes of bf16), sums by DPP and lane swaps.  The two halves of a
-// rotated pair lie in one lane (interleaved) or in lanes rot / 16 apart.  A
-// block takes a few steps and all their heads, so each angle is computed once
-// per step, not per head: the turn position * inv_freq / 2 pi in f64, reduced
-// to [-1/2, 1/2] there, then sine and cosine in f32.
+// elements a lane in two runs of four.  In the rotated part of a vector whose
+// pairs are (i, i + rot / 2) a lane's runs are the two halves of the same four
+// pairs, elsewhere they follow each other, so a rotation never leaves the lane
+// and reads four cosines and sines.  Sums go by DPP.  A block takes a few steps
+// and all their heads, so each angle is computed once per step, not per head: the
+// turn position * inv_freq / 2 pi in f64, reduced to [-1/2, 1/2] there, then sine
+// and cosine in f32.
 #include "pgf_gdr.h"
 #include "pgf_timing.h"
 
@@ -19,7 +21,6 @@ namespace qk {
 
 using gdr::View;
 using gdr::floatx4;
-using gdr::bf16x8;
 
 struct Args {
     View x[2], y[2], dy[2];          // q and k
@@ -35,158 +36,172 @@ struct Args {
     float *part;                     // [blocks][2][d] partial sums of dw
 };
 
-template <typename T>
-__device__ __forceinline__ void load8(const T *p, float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        const bf16x8 x = *(const bf16x8 *)p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)x[i];
-    } else {
-        const floatx4 a = ((const floatx4 *)p)[0], b = ((const floatx4 *)p)[1];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = a[i];
-            v[4 + i] = b[i];
-        }
-    }
-}
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 2) {
-        bf16x8 x;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = (__bf16)v[i];
-        *(bf16x8 *)p = x;
-    } else {
-        ((floatx4 *)p)[0] = floatx4{v[0], v[1], v[2], v[3]};
-        ((floatx4 *)p)[1] = floatx4{v[4], v[5], v[6], v[7]};
-    }
-}
+using gdr::Raw4;
+using gdr::load4;
 
 // Sum over a group of G lanes, in every lane of it.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+    return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, false));
+}
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {
+    if constexpr (G > 1) v = add_dpp<0xB1>(v);     // lane ^ 1
+    if constexpr (G > 2) v = add_dpp<0x4E>(v);     // lane ^ 2: sums of quads
+    if constexpr (G > 4) v = add_dpp<0x141>(v);    // 7 - lane: the other quad's
+    if constexpr (G > 8) v = add_dpp<0x140>(v);    // 15 - lane: the other eight's
 #pragma unroll
-    for (int m = 1; m < G; m *= 2) v += __shfl_xor(v, m, 64);
+    for (int m = 16; m < G; m *= 2) v += __shfl_xor(v, m, 64);
     return v;
 }
 
 constexpr int kPairs = 256;          // rotated pairs of a step at most
 constexpr int kTurn = 8;             // steps per block and turn at most
 
-// Rotation of a lane's eight elements (sgn = -1: back).  cs: cosine and sine
-// of the step's pairs.
-template <int G>
-__device__ __forceinline__ void rotate(float (&v)[8], const float2 *cs, int e0, int rot, int il, float sgn) {
-    if (il) {
-        if (e0 < rot) {
+// Rotation of a lane's runs (sgn = -1: back); cs: of its four pairs.
+__device__ __forceinline__ void rotate(floatx4 &x, floatx4 &y, const float2 *cs, int il, float sgn) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float2 t = cs[(e0 + i) / 2];
-                const float a = v[i], b = v[i + 1], s = sgn * t.y;
-                v[i] = a * t.x - b * s;
-                v[i + 1] = b * t.x + a * s;
-            }
-        }
-        return;
-    }
-    const int half = rot / 2, hl = half / 8;       // lanes from one element of a pair to the other
-    const int lane = threadIdx.x % 64;
-    const bool first = e0 < half, in = e0 < rot;
-    const int other = in ? (first ? lane + hl : lane - hl) : lane;
-    const int at = in ? (first ? e0 : e0 - half) : 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float o = __shfl(v[i], other, 64);
-        if (in) {
-            const float2 t = cs[at + i];
-            const float s = (first ? -sgn : sgn) * t.y;
-            v[i] = v[i] * t.x + o * s;
+    for (int i = 0; i < 4; ++i) {
+        const float c = cs[i].x, s = sgn * cs[i].y;
+        if (il) {                    // pairs (x0, x1), (x2, x3), (y0, y1), (y2, y3)
+            floatx4 &v = i < 2 ? x : y;
+            const float a = v[2 * (i & 1)], b = v[2 * (i & 1) + 1];
+            v[2 * (i & 1)] = a * c - b * s;
+            v[2 * (i & 1) + 1] = b * c + a * s;
+        } else {                     // pairs (x_i, y_i)
+            const float a = x[i], b = y[i];
+            x[i] = a * c - b * s;
+            y[i] = b * c + a * s;
         }
     }
 }
 
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const floatx4 &v) {
+    Raw4<T> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.x[i] = (T)v[i];
+    *(Raw4<T> *)p = r;
+}
+
 // Bound by memory: x is read and y written once (and dy read by the adjoint).
+// The next vector is loaded while one is computed, the first ones while the
+// angles are.
 template <typename T, int G, bool GRAD>
-__global__ __launch_bounds__(256) void k_qk(Args a) {
-    __shared__ float2 sCs[kTurn * kPairs];
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void k_qk(Args a) {
+    __shared__ __align__(16) float2 sCs[kTurn * kPairs];
     __shared__ float sW[GRAD ? 2 * 512 : 1];
     __shared__ int64_t sBT[kTurn][2];              // batch entry and step
     constexpr int NG = 256 / G;                    // head vectors at a time
-    const int tid = threadIdx.x, grp = tid / G, e0 = tid % G * 8;
-    const bool on = e0 < a.d;
+    const int tid = threadIdx.x, grp = tid / G, li = tid % G;
+    const bool on = 8 * li < a.d, turned = 8 * li < a.rot;
     const int half = a.rot / 2;
-    float w[2][8], dw[2][8];
+    // the lane's runs of elements, and its pairs
+    const int e0 = turned && !a.il ? 4 * li : 8 * li, e1 = turned && !a.il ? half + 4 * li : 8 * li + 4;
+    floatx4 w[2][2], dw[2][2];
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            w[x][i] = a.w[x] && on ? a.w[x][e0 + i] : 1.0f;
-            dw[x][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) {
+            w[x][0][i] = a.w[x] && on ? a.w[x][e0 + i] : 1.0f;
+            w[x][1][i] = a.w[x] && on ? a.w[x][e1 + i] : 1.0f;
+            dw[x][0][i] = dw[x][1][i] = 0.0f;
         }
+    struct Unit {
+        Raw4<T> x[2], g[GRAD ? 2 : 1];
+    };
     for (int64_t r0 = (int64_t)blockIdx.x * a.tb; r0 < a.rows; r0 += (int64_t)gridDim.x * a.tb) {
         const int nt = (int)(a.rows - r0 < a.tb ? a.rows - r0 : a.tb);
+        const int units = nt * a.H;
         __syncthreads();
         if (tid < nt) {
             sBT[tid][0] = (r0 + tid) / a.L;
             sBT[tid][1] = (r0 + tid) - sBT[tid][0] * a.L;
         }
         __syncthreads();
+        // place of unit u (a lane without one repeats the last, and does not store)
+        int s, x, h;
+        int64_t b, t;
+        auto place = [&](int u) {
+            u = u < units ? u : units - 1;
+            s = u / a.H;
+            h = u - s * a.H;
+            x = h >= a.H0;                         // 0 = query, 1 = key
+            h -= x ? a.H0 : 0;
+            b = sBT[s][0];
+            t = sBT[s][1];
+        };
+        auto fetch = [&](int u) {
+            place(u);
+            Unit v;
+            const T *p = (x ? a.x[1] : a.x[0]).template at<const T>(b, h, t);
+            const int f0 = on ? e0 : 0, f1 = on ? e1 : 0;
+            v.x[0] = load4(p + f0);
+            v.x[1] = load4(p + f1);
+            if constexpr (GRAD) {
+                const T *q = (x ? a.dy[1] : a.dy[0]).template at<const T>(b, h, t);
+                v.g[0] = load4(q + f0);
+                v.g[1] = load4(q + f1);
+            }
+            return v;
+        };
+        Unit next = fetch(grp);
         if (a.rot) {
             for (int i = tid; i < nt * half; i += 256) {
-                const int64_t b = sBT[i / half][0], t = sBT[i / half][1];
-                const int64_t at = b * a.pos_stride + t;
-                const double pos = !a.pos ? (double)t : a.pos64 ? (double)((const int64_t *)a.pos)[at]
-                                                                : (double)((const int32_t *)a.pos)[at];
+                const int64_t at = sBT[i / half][0] * a.pos_stride + sBT[i / half][1];
+                const double pos = !a.pos ? (double)sBT[i / half][1] : a.pos64 ? (double)((const int64_t *)a.pos)[at]
+                                                                               : (double)((const int32_t *)a.pos)[at];
                 double turns = pos * (double)a.inv_freq[i % half] * 0.15915494309189533577;   // 1 / 2 pi
                 turns -= rint(turns);
-                float s, c;
-                sincospif(2.0f * (float)turns, &s, &c);
-                sCs[i] = float2{c, s};
+                float sn, cn;
+                sincospif(2.0f * (float)turns, &sn, &cn);
+                sCs[i] = float2{cn, sn};
             }
             __syncthreads();
         }
-        const int units = nt * a.H;
         for (int u0 = 0; u0 < units; u0 += NG) {
-            const int u = u0 + grp;
-            const bool live = u < units;           // lanes of one group agree
-            const int s = live ? u / a.H : 0, hh = live ? u - s * a.H : 0;
-            const int x = hh >= a.H0;              // 0 = query, 1 = key
-            const int h = x ? hh - a.H0 : hh;
-            const int64_t b = sBT[s][0], t = sBT[s][1];
-            const bool act = live && on;
-            float v[8] = {};
-            if (act) load8((x ? a.x[1] : a.x[0]).template at<const T>(b, h, t) + e0, v);
+            const Unit cur = next;
+            next = fetch(u0 + NG + grp);
+            place(u0 + grp);
+            const bool live = u0 + grp < units, act = live && on;      // lanes of one group agree on live
+            floatx4 v0 = cur.x[0].f(), v1 = cur.x[1].f();
             float ss = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
-            ss = group_sum<G>(ss);
+            for (int i = 0; i < 4; ++i) ss = fmaf(v0[i], v0[i], fmaf(v1[i], v1[i], ss));
+            ss = group_sum<G>(on ? ss : 0.0f);
             const float rs = a.c == 0.0f ? 1.0f : 1.0f / sqrtf(fmaf(ss, a.c, a.eps));
-            const float2 *cs = sCs + s * half;
+            const float2 *cs = sCs + s * half + 4 * li;
+            T *out = (x ? a.y[1] : a.y[0]).template at<T>(b, h, t);
+            const floatx4 w0 = x ? w[1][0] : w[0][0], w1 = x ? w[1][1] : w[0][1];
             if constexpr (!GRAD) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = v[i] * rs * (x ? w[1][i] : w[0][i]);
-                if (a.rot) rotate<G>(v, cs, e0, a.rot, a.il, 1.0f);
-                if (act) store8((x ? a.y[1] : a.y[0]).template at<T>(b, h, t) + e0, v);
+                v0 = v0 * rs * w0;
+                v1 = v1 * rs * w1;
+                if (turned) rotate(v0, v1, cs, a.il, 1.0f);
             } else {
-                float g[8] = {};
-                if (act) load8((x ? a.dy[1] : a.dy[0]).template at<const T>(b, h, t) + e0, g);
-                if (a.rot) rotate<G>(g, cs, e0, a.rot, a.il, -1.0f);
+                floatx4 g0 = cur.g[0].f(), g1 = cur.g[1].f();
+                if (turned) rotate(g0, g1, cs, a.il, -1.0f);
+                const floatx4 d0 = g0 * (v0 * rs), d1 = g1 * (v1 * rs);
+                if (live) {
+                    if (x) {
+                        dw[1][0] += d0;
+                        dw[1][1] += d1;
+                    } else {
+                        dw[0][0] += d0;
+                        dw[0][1] += d1;
+                    }
+                }
+                g0 *= w0;
+                g1 *= w1;
                 float dot = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float xr = g[i] * (v[i] * rs);
-                    if (live) {
-                        dw[0][i] += x ? 0.0f : xr;
-                        dw[1][i] += x ? xr : 0.0f;
-                    }
-                    g[i] *= x ? w[1][i] : w[0][i];
-                    dot = fmaf(v[i], g[i], dot);
-                }
-                dot = group_sum<G>(dot) * (rs * rs * a.c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = rs * (g[i] - v[i] * dot);
-                if (act) store8((x ? a.y[1] : a.y[0]).template at<T>(b, h, t) + e0, v);
+                for (int i = 0; i < 4; ++i) dot = fmaf(v0[i], g0[i], fmaf(v1[i], g1[i], dot));
+                dot = group_sum<G>(on ? dot : 0.0f) * (rs * rs * a.c);
+                v0 = rs * (g0 - v0 * dot);
+                v1 = rs * (g1 - v1 * dot);
+            }
+            if (act) {
+                store4(out + e0, v0);
+                store4(out + e1, v1);
             }
         }
     }
@@ -196,20 +211,23 @@ __global__ __launch_bounds__(256) void k_qk(Args a) {
 #pragma unroll
         for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float v = dw[x][i];
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int m = G; m < 64; m *= 2) v += __shfl_xor(v, m, 64);
-                dw[x][i] = v;
-            }
+                for (int i = 0; i < 4; ++i) {
+                    float v = dw[x][k][i];
+#pragma unroll
+                    for (int m = G; m < 64; m *= 2) v += __shfl_xor(v, m, 64);
+                    dw[x][k][i] = v;
+                }
         for (int wv = 0; wv < 4; ++wv) {
             if (tid / 64 == wv && tid % 64 < G && on) {
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float &s = sW[x * 512 + e0 + i];
-                        s = wv ? s + dw[x][i] : dw[x][i];
+                    for (int i = 0; i < 4; ++i) {
+                        float &s0 = sW[x * 512 + e0 + i], &s1 = sW[x * 512 + e1 + i];
+                        s0 = wv ? s0 + dw[x][0][i] : dw[x][0][i];
+                        s1 = wv ? s1 + dw[x][1][i] : dw[x][1][i];
                     }
             }
             __syncthreads();
@@ -221,17 +239,25 @@ __global__ __launch_bounds__(256) void k_qk(Args a) {
     }
 }
 
-// dw of one element of the query's (x = 0) or key's weight: the blocks'
-// partial sums, a fixed share per lane, then over the lanes.
-__global__ __launch_bounds__(64) void k_qk_dw(const float *part, int blocks, int d, float *dwq, float *dwk) {
-    const int e = blockIdx.x, x = e >= d;
-    float *out = x ? dwk : dwq;
-    if (!out) return;
+// dw of 32 elements (the query's weight, then the key's): 32 threads an element
+// sum a fixed share of the blocks' partial sums each, and then each other's.
+__global__ __launch_bounds__(1024) void k_qk_dw(const float *part, int blocks, int d, float *dwq, float *dwk) {
+    __shared__ float sS[32][33];
+    const int c = threadIdx.x % 32, g = threadIdx.x / 32;
+    const int e = blockIdx.x * 32 + c;
     float s = 0.0f;
-    for (int b = threadIdx.x; b < blocks; b += 64) s += part[(int64_t)b * 2 * d + e];
+    if (e < 2 * d) {
+#pragma unroll 4
+        for (int b = g; b < blocks; b += 32) s += part[(int64_t)b * 2 * d + e];
+    }
+    sS[g][c] = s;
+    __syncthreads();
+    s = sS[c][g];                                  // element g of the 32, share c
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) s += __shfl_xor(s, m, 64);
-    if (threadIdx.x == 0) out[x ? e - d : e] = s;
+    for (int m = 1; m < 32; m *= 2) s += __shfl_xor(s, m, 32);
+    const int o = blockIdx.x * 32 + g, x = o >= d;
+    float *out = x ? dwk : dwq;
+    if (c == 0 && o < 2 * d && out) out[x ? o - d : o] = s;
 }
 
 View view(const void *p, const int64_t (&s)[3], int64_t H, int64_t L, int64_t d) {
@@ -317,11 +343,12 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
     a.H = (int)(pl.Hq + pl.Hk);
     a.eps = p->eps;
     a.c = p->norm == PGF_NORM_NONE ? 0.0f : p->norm == PGF_NORM_L2 ? 1.0f : 1.0f / (float)pl.d;
-    // Steps per block: one while that leaves the GPU idle, then as many as fill
-    // a few turns of the block's head groups.
-    const int64_t per = 256 / pl.G;
+    // Steps per block: one while that leaves CUs without a few blocks, then as
+    // many as keep those (a block's start, with its angles, costs as much as a
+    // few vectors a lane: 16384 steps of 32 heads, two steps a block 112 us,
+    // eight 66).
     a.tb = 1;
-    while (a.tb < kTurn && a.tb * a.H < 4 * per && a.rows / (2 * a.tb) >= 1024) a.tb *= 2;
+    while (a.tb < kTurn && a.rows / (2 * a.tb) >= 1024) a.tb *= 2;
     const int64_t want = (a.rows + a.tb - 1) / a.tb;
     const bool bf = p->in_dtype == PGF_BF16;
     if (!grads) {
@@ -339,7 +366,7 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
         }
         if (a.part) {
             Timed tm(2, st);
-            hipLaunchKernelGGL(k_qk_dw, dim3((unsigned)(2 * pl.d)), dim3(64), 0, st, (const float *)a.part, (int)blocks,
+            hipLaunchKernelGGL(k_qk_dw, dim3((unsigned)((2 * pl.d + 31) / 32)), dim3(1024), 0, st, (const float *)a.part, (int)blocks,
                                (int)pl.d, p->w_q ? p->grad_w_q : nullptr, p->w_k ? p->grad_w_k : nullptr);
         }
     }
