@@ -625,15 +625,14 @@ def _rows(t, shape, dev, dtype, name):
     is copied."""
     if t.dtype is not dtype or t.shape != shape or t.device != dev:
         _bad(t, shape, dev, dtype, name)
-    B, H, L = shape[:3]
     st = t.stride()
-    sb, sh, sl = st[0] if B > 1 else 0, st[1] if H > 1 else 0, st[2] if L > 1 else 0
+    sb, sh, sl = st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0
     if len(shape) == 4:
-        unit = 8 if dtype is torch.bfloat16 else 4
-        ok = (st[3] == 1 or shape[3] == 1) and not ((sb | sh | sl) % unit or t.data_ptr() % 16)
+        unit = 7 if dtype is torch.bfloat16 else 3
+        ok = not ((sb | sh | sl) & unit or t.data_ptr() & 15) and (st[3] == 1 or shape[3] == 1)
     else:
         ok = True
-    if not ((ok and (sb or sh or sl or B * H * L <= 1)) or t.numel() == 0):
+    if not (ok and (sb or sh or sl or shape[0] * shape[1] * shape[2] <= 1)) and t.numel():
         return _rows(t.clone(memory_format=torch.contiguous_format), shape, dev, dtype, name)
     return t, (sb, sh, sl)
 
@@ -691,8 +690,12 @@ def _on(dev, stream):
     return stack
 
 
+# The current stream's handle without a Stream object around it, where torch has that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream_of(dev):
-    return torch.cuda.current_stream(dev).cuda_stream
+    return _raw_stream(dev.index) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
 
 
 def _on_device(names, *ts):

@@ -208,15 +208,19 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
             s.ct = a.vt + (int)((pl.dk + 15) / 16);
             const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment>), dim3(xcd_grid(items, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, items);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment, 1>), dim3(xcd_grid(items, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, items);
         }
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt)), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt)), dim3(4 * DK), 0, st, a);
         a.seg_in = a.segE;
     }
-    const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
     Timed tm(3, st);
-    hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut>), dim3(xcd_grid(items, (a.ct + 3) / 4 * a.rep)), dim3(256), 0, st, a, items);
+    const int share = pl.seg_slots * pl.Hv * a.ct <= kShareWaves ? 2 : 1;
+    const int cb = (a.ct + 4 / share - 1) / (4 / share);
+    const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * cb);
+    const dim3 grid(xcd_grid(items, cb * a.rep));
+    if (share == 2) hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut, 2>), grid, dim3(256), 0, st, a, items);
+    else hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut, 1>), grid, dim3(256), 0, st, a, items);
     return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;
 }
 

@@ -256,24 +256,33 @@ struct Chunk {
     __align__(16) float eG[32];
 };
 
-template <typename T, int DK, int MODE>
+constexpr int64_t kShareWaves = 768;         // waves of column tiles up to which waves share one
+// HS = 2: two waves share a column tile, each with half of the keys; they add
+// their parts of K S and Q S through LDS and both go on from the sum, each
+// updating its keys and writing half the outputs.  A fifth more work for half the
+// chain: taken where one wave a tile leaves SIMDs idle or alone with one wave
+// (which issues only half the instructions two can).
+template <typename T, int DK, int MODE, int HS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_chain(Args a, uint32_t n_items) {
     using Ck = Chunk<T, DK, MODE>;
     constexpr int P = Ck::P, PO = Ck::PO, NI = Ck::NI;
     constexpr bool OUT = MODE == kOut;
-    constexpr int KS = DK / 32, KT = DK / 16;
-    constexpr int KU = 32 * DK / 8 / 256;          // 8-key units of K a thread stages (and of Q)
-    constexpr int MU = (NI * 128 + 255) / 256;     // 16-byte units of the images
+    constexpr int NT = 256, TB = 4 / HS;           // threads, column tiles
+    constexpr int KS = DK / 32 / HS, KT = DK / 16 / HS;    // of this wave's keys
+    constexpr int UNITS = 32 * DK / 8;             // 8-key units of K (and of Q)
+    constexpr int KU = (UNITS + NT - 1) / NT;      // those a thread stages
+    constexpr int MU = (NI * 128 + NT - 1) / NT;   // 16-byte units of the images
     // Two chunks in LDS where a CU still holds two blocks (one barrier a chunk).
     constexpr int NB = sizeof(Ck) <= 40960 ? 2 : 1;
     __shared__ Ck lds[NB];
+    __shared__ floatx4 sEx[HS > 1 ? HS : 1][HS > 1 ? TB : 1][4][HS > 1 ? 64 : 1];      // [half][tile][K S, Q S][lane]
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
-    const int w = __builtin_amdgcn_readfirstlane(tid / 64);
-    const int cb = (a.ct + 3) / 4;                 // blocks of a head
+    const int wv = __builtin_amdgcn_readfirstlane(tid / 64), w = wv % TB, hh = wv / TB;
+    const int cb = (a.ct + TB - 1) / TB;           // blocks of a head
     const uint32_t item = xcd_item(blockIdx.x, (uint32_t)(cb * a.rep));
     if (item >= n_items) return;
     const int64_t sh = item / cb;
-    const int tile = (int)(item - sh * cb) * 4 + w;
+    const int tile = (int)(item - sh * cb) * TB + w;
     const int64_t slot = sh / a.Hv;
     const int h = (int)(sh - slot * a.Hv), hk = h / a.rep;
     const Rows r = a.seqs.of(slot, a.seg ? a.seg : a.seqs.L + 1, a.seg_per);
@@ -294,7 +303,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         MODE == kSave ? uni(a.seqs.slot0(r.n, kC * a.save, a.save_per) + r.unit0 / (kC * a.save)) : 0;
 
     // S[kt][j]: key key0(kt) + j of this lane's column
-    auto key0 = [&](int kt) { return 32 * (kt / 2) + 8 * qd + 4 * (kt & 1); };
+    auto key0 = [&](int kt) { return 32 * (hh * KS + kt / 2) + 8 * qd + 4 * (kt & 1); };
     floatx4 S[KT];
     {
         const float *in = MODE == kSegment ? nullptr : a.seg_in && r.len ? a.seg_in + (slot * a.Hv + h) * a.dk * a.dv
@@ -346,9 +355,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     uint32_t ko[KU], qo[KU];
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
-        const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
-        ko[i] = e < a.dk ? t * kst + e * (uint32_t)sizeof(T) : kNone;
-        qo[i] = e < a.dk ? t * qst + e * (uint32_t)sizeof(T) : kNone;
+        const int u = tid + NT * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
+        const bool on = e < a.dk && u < UNITS;
+        ko[i] = on ? t * kst + e * (uint32_t)sizeof(T) : kNone;
+        qo[i] = on ? t * qst + e * (uint32_t)sizeof(T) : kNone;
     }
     auto live_rows = [&](int ch) {
         const int64_t left = n - (int64_t)ch * kC;
@@ -367,7 +377,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         const char *rec = a.rec + ((slot0 + ch) * a.Hv + h) * (int64_t)rb;
 #pragma unroll
         for (int i = 0; i < MU; ++i) {
-            const int u = tid + 256 * i < NI * 128 ? tid + 256 * i : tid;
+            const int u = tid + NT * i < NI * 128 ? tid + NT * i : tid % 128;
             rm[i] = *(const uintx4 *)(rec + (MODE == kSave && u >= 384 ? rec_rows(rp) + 256 - 384 * 16 : 0u) + 16u * u);
         }
         reG = *(const float *)(rec + rec_rows(rp) + 4 * (tid % 32));
@@ -379,7 +389,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     auto stage = [&](Ck &s) {
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
-            const int u = tid + 256 * i, t = u / (DK / 8);
+            const int u = tid + NT * i, t = u / (DK / 8);
+            if (64 * wv + NT * i >= UNITS) continue;
             const uint32_t at = unit_off<DK>(t, u % (DK / 8));
             const Frag<P> f = raw_frag<P>(rk[i]);
 #pragma unroll
@@ -392,7 +403,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
 #pragma unroll
         for (int i = 0; i < MU; ++i)
-            if (64 * w + 256 * i < NI * 128) *(uintx4 *)(&s.M[0][0] + 16 * (tid + 256 * i)) = rm[i];
+            if (64 * wv + NT * i < NI * 128) *(uintx4 *)(&s.M[0][0] + 16 * (tid + NT * i)) = rm[i];
         if (tid < 32) s.eG[tid] = reG;
     };
 
@@ -412,7 +423,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             for (int j = 0; j < 4; ++j) vv[m][j] = raw_f<T>(rv[m][j]);
         const Ck &s = lds[NB == 2 ? ch & 1 : 0];
         fetch(ch + 1 < chunks ? ch + 1 : ch);      // (the last chunk again rather than a branch)
-        if (mine) {
+        if (HS > 1 || mine) {                      // (waves that share barriers go through the motions)
             // Operands are read a step ahead of their products: left to
             // itself the compiler reads each where it is needed and waits.
             floatx4 kS[2], qS[2];
@@ -424,7 +435,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
-                        const uint32_t at = unit_off<DK>(16 * m + c, 4 * ks + qd);
+                        const uint32_t at = unit_off<DK>(16 * m + c, 4 * (hh * KS + ks) + qd);
                         kf[ks & 1][m].p[p] = *(const bf16x8 *)&s.K[p][at];
                         if constexpr (OUT) qf[ks & 1][m].p[p] = *(const bf16x8 *)&s.Q[p][at];
                     }
@@ -453,6 +464,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 if constexpr (OUT) mfma_parts2<P, PO>(qf[ks & 1], so, qS);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            if constexpr (HS > 1) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    sEx[hh][w][m][lane] = kS[m];
+                    if constexpr (OUT) sEx[hh][w][2 + m][lane] = qS[m];
+                }
+                lds_barrier();
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    kS[m] = sEx[0][w][m][lane] + sEx[1][w][m][lane];
+                    if constexpr (OUT) qS[m] = sEx[0][w][2 + m][lane] + sEx[1][w][2 + m][lane];
+                }
+            }
             floatx4 X[2];
 #pragma unroll
             for (int m = 0; m < 2; ++m)
@@ -462,12 +486,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                     if constexpr (OUT) qS[m][j] *= eG[m][j];
                 }
             const Frag<3> xp = to_frag<3>(X[0], X[1]);
-            constexpr int GK = P == 1 ? 4 : 2;     // key tiles read at a time
+            constexpr int GK = P == 1 && KT >= 4 ? 4 : 2;     // key tiles read at a time
             Frag<P> ktf[2][GK];
             auto read_kt = [&](int g) {
 #pragma unroll
                 for (int i = 0; i < GK; ++i) {
-                    const int kt = g * GK + i, row = 4 * qd + c / 4;
+                    const int kt = hh * KT + g * GK + i, row = 4 * qd + c / 4;
 #pragma unroll
                     for (int p = 0; p < P; ++p) {
                         const char *k0 = &s.K[p][unit_off<DK>(row, 4 * (kt / 2) + c % 4) + 8 * (kt & 1)];
@@ -514,17 +538,23 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
                 for (int p = 0; p < PO; ++p) xo.p[p] = xp.p[p];
                 const Buf ob = make_buf(op + (int64_t)ch * kC * a.o.st, ost, live_rows(ch), a.dv * (int)sizeof(T));
-                mfma_parts2<PO, PO>(af, xo, qS);
+                if constexpr (HS > 1) {            // (rows 16 hh ..)
+                    const floatx4 o = mfma_parts<PO, PO>(hh ? af[1] : af[0], xo, hh ? qS[1] : qS[0]);
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
+                    for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * hh + j) * ost, o[j] * a.scale);
+                } else {
+                    mfma_parts2<PO, PO>(af, xo, qS);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * m + j) * ost, qS[m][j] * a.scale);
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * m + j) * ost, qS[m][j] * a.scale);
+                }
             }
             if constexpr (MODE == kSave) {
                 float *eb = a.saveE + ((slot0 + ch) * a.Hv + h) * (int64_t)(kC * a.dv);
                 floatx4 e[2] = {};
                 mfma_parts2<3, 3>(af, xp, e);
-                if (live_col) {
+                if (live_col && hh == 0) {
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -561,7 +591,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // About 1 us a segment: its products wait for the last segment's.
 template <int DK, bool BACK>
 __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile, char (*sS)[16 * DK * 2]) {
-    constexpr int KS = DK / 32, MT = DK / 64;      // (key tiles of a wave)
+    constexpr int KS = DK / 32, MT = 1;            // key tiles of a wave
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t slot0 = uni(a.seqs.slot0(n, a.seg, a.seg_per));
@@ -573,13 +603,15 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
     float *E = BACK ? a.dsegE : a.segE;
     const float *M = BACK ? a.trT : a.tr;
     const int64_t cell = a.dk * a.dv;
-    floatx4 S[MT], e[MT];
-    Raw8<float> mr[MT][KS];
+    constexpr int D = 3;                           // segments loaded ahead
+    floatx4 S[MT], es[D][MT];
+    Raw8<float> mrs[D][MT][KS];
     auto offs = [&](int m) {                       // of this lane's four keys in a state
         const int key = 16 * (MT * w + m) + 4 * qd;
         return on && key < a.dk ? (uint32_t)(key * a.dv + col) * 4u : kNone;
     };
-    auto fetch = [&](int g) {
+    auto fetch = [&](int g, floatx4 (&e)[MT], Raw8<float> (&mr)[MT][KS]) {
+        g = g < G ? g : G - 1;
         const int64_t at = (slot0 + (BACK ? G - 1 - g : g)) * a.Hv + h;
         const Buf eb = make_buf((const void *)uni((int64_t)(uintptr_t)(E + at * cell)), a.dv * 4, a.dk, a.dv * 4);
         const Buf mb = make_buf((const void *)uni((int64_t)(uintptr_t)(M + at * DK * DK)), DK * 4, a.dk, a.dk * 4);
@@ -602,8 +634,10 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
 #pragma unroll
             for (int j = 0; j < 4; ++j) S[m][j] = raw_f<float>(load1<float>(ib, offs(m), j * ib.st));
     }
-    if (G > 0) fetch(0);
-    for (int g = 0; g < G; ++g) {
+    if (G == 0) return;
+#pragma unroll
+    for (int u = 0; u < D; ++u) fetch(u, es[u], mrs[u]);
+    auto step = [&](int g, floatx4 (&e)[MT], Raw8<float> (&mr)[MT][KS]) {
         const int64_t at = (slot0 + (BACK ? G - 1 - g : g)) * a.Hv + h;
         char *buf = &sS[3 * (g & 1)][0];
         floatx4 acc[MT];
@@ -615,16 +649,17 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
             const int key = 16 * (MT * w + m) + 4 * qd;
 #pragma unroll
             for (int p = 0; p < 3; ++p) *(bf16x4 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, key / 8) + 2 * (key & 4)] = x[p];
-            acc[m] = e[m];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) mf[m][ks] = raw_frag<3>(mr[m][ks]);
         }
         const Buf eb = make_buf((const void *)uni((int64_t)(uintptr_t)(E + at * cell)), a.dv * 4, a.dk, a.dv * 4);
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int m = 0; m < MT; ++m) {
+            acc[m] = e[m];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) mf[m][ks] = raw_frag<3>(mr[m][ks]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) store1<float>(eb, offs(m), j * eb.st, S[m][j]);
-        if (g + 1 < G) fetch(g + 1);
+        }
+        fetch(g + D, e, mr);
         lds_barrier();
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
@@ -636,12 +671,16 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m) S[m] = acc[m];
-    }
+    };
+    for (int g0 = 0; g0 < G; g0 += D)
+#pragma unroll
+        for (int u = 0; u < D; ++u)
+            if (g0 + u < G) step(g0 + u, es[u], mrs[u]);
 }
 
 // BOTH: the adjoint's carry beside the state's (blockIdx.y).
 template <int DK, bool BOTH>
-__global__ __launch_bounds__(256) void k_gdr_carry(Args a) {
+__global__ __launch_bounds__(4 * DK) void k_gdr_carry(Args a) {
     __shared__ __align__(16) char sS[6][16 * DK * 2];      // two states of three parts, by column
     const int64_t nh = blockIdx.x / a.vt;
     const int tile = (int)(blockIdx.x - nh * a.vt);
