@@ -211,7 +211,7 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
             hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment, 1>), dim3(xcd_grid(items, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, items);
         }
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt)), dim3(4 * DK), 0, st, a);
+        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3(xcd_grid(pl.nseq * pl.Hv * a.vt, a.vt)), dim3(4 * DK), 0, st, a);
         a.seg_in = a.segE;
     }
     Timed tm(3, st);

@@ -591,101 +591,94 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // About 1 us a segment: its products wait for the last segment's.
 template <int DK, bool BACK>
 __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile, char (*sS)[16 * DK * 2]) {
-    constexpr int KS = DK / 32, MT = 1;            // key tiles of a wave
+    constexpr int KS = DK / 32, D = 3;             // segments loaded ahead
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
     const int w = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t slot0 = uni(a.seqs.slot0(n, a.seg, a.seg_per));
     const int64_t len = a.seqs.cu ? (a.seqs.bound(n + 1) > a.seqs.bound(n) ? a.seqs.bound(n + 1) - a.seqs.bound(n) : 0) : a.seqs.L;
     const int G = (int)uni((len + a.seg - 1) / a.seg);
-    const int col = 16 * tile + c;
-    const bool on = col < a.dv;
-    const float *init = BACK ? a.dS_out : a.S_in;
-    float *E = BACK ? a.dsegE : a.segE;
-    const float *M = BACK ? a.trT : a.tr;
-    const int64_t cell = a.dk * a.dv;
-    constexpr int D = 3;                           // segments loaded ahead
-    floatx4 S[MT], es[D][MT];
-    Raw8<float> mrs[D][MT][KS];
-    auto offs = [&](int m) {                       // of this lane's four keys in a state
-        const int key = 16 * (MT * w + m) + 4 * qd;
-        return on && key < a.dk ? (uint32_t)(key * a.dv + col) * 4u : kNone;
-    };
-    auto fetch = [&](int g, floatx4 (&e)[MT], Raw8<float> (&mr)[MT][KS]) {
-        g = g < G ? g : G - 1;
-        const int64_t at = (slot0 + (BACK ? G - 1 - g : g)) * a.Hv + h;
-        const Buf eb = make_buf((const void *)uni((int64_t)(uintptr_t)(E + at * cell)), a.dv * 4, a.dk, a.dv * 4);
-        const Buf mb = make_buf((const void *)uni((int64_t)(uintptr_t)(M + at * DK * DK)), DK * 4, a.dk, a.dk * 4);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) e[m][j] = raw_f<float>(load1<float>(eb, offs(m), j * eb.st));
-            const int key = 16 * (MT * w + m) + c;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                mr[m][ks] = load8<float>(mb, key < a.dk && 32 * ks + 8 * qd < a.dk ? key * mb.st + (32 * ks + 8 * qd) * 4u : kNone, 0);
-        }
-    };
-#pragma unroll
-    for (int m = 0; m < MT; ++m) S[m] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    if (init) {
-        const Buf ib = make_buf((const void *)uni((int64_t)(uintptr_t)(init + (n * a.Hv + h) * cell)), a.dv * 4, a.dk, a.dv * 4);
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) S[m][j] = raw_f<float>(load1<float>(ib, offs(m), j * ib.st));
-    }
     if (G == 0) return;
+    const int col = 16 * tile + c, key = 16 * w + 4 * qd, row = 16 * w + c;
+    const int64_t cell = a.dk * a.dv;
+    const float *init = BACK ? a.dS_out : a.S_in;
+    // segment g's arrays: `step` segments of all heads apart, from the first one taken
+    const int64_t first = (slot0 + (BACK ? G - 1 : 0)) * a.Hv + h;
+    const int64_t dE = (BACK ? -1 : 1) * (int64_t)a.Hv * cell, dM = (BACK ? -1 : 1) * (int64_t)a.Hv * (DK * DK);
+    float *E = (float *)uni((int64_t)(uintptr_t)((BACK ? a.dsegE : a.segE) + first * cell));
+    const float *M = (const float *)uni((int64_t)(uintptr_t)((BACK ? a.trT : a.tr) + first * (DK * DK)));
+    const uint32_t est = a.dv * 4, ebytes = a.dk * est;
+    const uint32_t so = col < a.dv && key < a.dk ? (uint32_t)(key * a.dv + col) * 4u : kNone;    // this lane's four keys
+    uint32_t mo[KS];                               // its row of M
 #pragma unroll
-    for (int u = 0; u < D; ++u) fetch(u, es[u], mrs[u]);
-    auto step = [&](int g, floatx4 (&e)[MT], Raw8<float> (&mr)[MT][KS]) {
-        const int64_t at = (slot0 + (BACK ? G - 1 - g : g)) * a.Hv + h;
-        char *buf = &sS[3 * (g & 1)][0];
-        floatx4 acc[MT];
-        Frag<3> mf[MT][KS];
+    for (int ks = 0; ks < KS; ++ks)
+        mo[ks] = row < a.dk && 32 * ks + 8 * qd < a.dk ? (uint32_t)(row * DK + 32 * ks + 8 * qd) * 4u : kNone;
+    auto state = [&](const float *p) { return Buf{__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)ebytes, 0x00020000), est}; };
+    floatx4 S = {0.0f, 0.0f, 0.0f, 0.0f}, es[D];
+    Raw8<float> ms[D][KS];
+    auto fetch = [&](int g, floatx4 &e, Raw8<float> (&m)[KS]) {
+        g = g < G ? g : G - 1;
+        const Buf eb = state(E + g * dE);
+        const Buf mb{__builtin_amdgcn_make_buffer_rsrc((void *)(M + g * dM), 0, DK * DK * 4, 0x00020000), DK * 4};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            bf16x4 x[3];
-            split4<3>(S[m], x);
-            const int key = 16 * (MT * w + m) + 4 * qd;
+        for (int j = 0; j < 4; ++j) e[j] = raw_f<float>(load1<float>(eb, so, j * est));
 #pragma unroll
-            for (int p = 0; p < 3; ++p) *(bf16x4 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, key / 8) + 2 * (key & 4)] = x[p];
-        }
-        const Buf eb = make_buf((const void *)uni((int64_t)(uintptr_t)(E + at * cell)), a.dv * 4, a.dk, a.dv * 4);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            acc[m] = e[m];
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks) mf[m][ks] = raw_frag<3>(mr[m][ks]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) store1<float>(eb, offs(m), j * eb.st, S[m][j]);
-        }
-        fetch(g + D, e, mr);
-        lds_barrier();
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            Frag<3> sf;
-#pragma unroll
-            for (int p = 0; p < 3; ++p) sf.p[p] = *(const bf16x8 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, 4 * ks + qd)];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) acc[m] = mfma_parts<3, 3>(mf[m][ks], sf, acc[m]);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) S[m] = acc[m];
+        for (int ks = 0; ks < KS; ++ks) m[ks] = load8<float>(mb, mo[ks], 0);
     };
-    for (int g0 = 0; g0 < G; g0 += D)
+    if (init) {
+        const Buf ib = state((const float *)uni((int64_t)(uintptr_t)(init + (n * a.Hv + h) * cell)));
 #pragma unroll
-        for (int u = 0; u < D; ++u)
-            if (g0 + u < G) step(g0 + u, es[u], mrs[u]);
+        for (int j = 0; j < 4; ++j) S[j] = raw_f<float>(load1<float>(ib, so, j * est));
+    }
+#pragma unroll
+    for (int u = 0; u < D; ++u) fetch(u, es[u], ms[u]);
+    auto step = [&](int g, floatx4 &e, Raw8<float> (&m)[KS]) {
+        char *buf = &sS[3 * (g & 1)][0];
+        bf16x4 x[3];
+        split4<3>(S, x);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *(bf16x4 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, key / 8) + 2 * (key & 4)] = x[p];
+        const Buf eb = state(E + g * dE);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store1<float>(eb, so, j * est, S[j]);
+        floatx4 acc[2] = {e, {0.0f, 0.0f, 0.0f, 0.0f}};
+        Frag<3> mf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) mf[ks] = raw_frag<3>(m[ks]);
+        fetch(g + D, e, m);
+        lds_barrier();
+        Frag<3> sf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int p = 0; p < 3; ++p) sf[ks].p[p] = *(const bf16x8 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, 4 * ks + qd)];
+        // two sums in turn: a product waits for the last one of its sum
+#pragma unroll
+        for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+            for (int i = 0; i <= sum; ++i)
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) acc[ks & 1] = mfma(mf[ks].p[i], sf[ks].p[sum - i], acc[ks & 1]);
+        S = acc[0] + acc[1];
+    };
+    int g0 = 0;
+    for (; g0 + D <= G; g0 += D)       // (no condition between the steps: behind one, all loads would be waited for)
+#pragma unroll
+        for (int u = 0; u < D; ++u) step(g0 + u, es[u], ms[u]);
+#pragma unroll
+    for (int u = 0; u < D - 1; ++u)
+        if (g0 + u < G) step(g0 + u, es[u], ms[u]);
 }
 
 // BOTH: the adjoint's carry beside the state's (blockIdx.y).
 template <int DK, bool BOTH>
 __global__ __launch_bounds__(4 * DK) void k_gdr_carry(Args a) {
     __shared__ __align__(16) char sS[6][16 * DK * 2];      // two states of three parts, by column
-    const int64_t nh = blockIdx.x / a.vt;
-    const int tile = (int)(blockIdx.x - nh * a.vt);
+    const uint32_t item = xcd_item(blockIdx.x, (uint32_t)a.vt);      // (the tiles of a head read the same M)
+    const int64_t nh = item / (uint32_t)a.vt;
+    const int tile = (int)(item - nh * a.vt);
     const int64_t n = nh / a.Hv;
     const int h = (int)(nh - n * a.Hv);
+    if (n >= a.seqs.n) return;
     if (BOTH && blockIdx.y) carry<DK, true>(a, n, h, tile, sS);
     else carry<DK, false>(a, n, h, tile, sS);
 }

@@ -723,7 +723,7 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
             hipLaunchKernelGGL((k_gdr_back<T, DK, kBackSegment>), dim3(xcd_grid(n, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, n);
         }
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_carry<DK, true>), dim3((unsigned)(pl.nseq * pl.Hv * a.vt), 2), dim3(4 * DK), 0, st, a);
+        hipLaunchKernelGGL((k_gdr_carry<DK, true>), dim3(xcd_grid(pl.nseq * pl.Hv * a.vt, a.vt), 2), dim3(4 * DK), 0, st, a);
         a.seg_in = a.segE;
         a.dseg_in = a.dsegE;
     }

@@ -80,7 +80,7 @@ int64_t default_seg(const Plan &q, bool packed) {
     const double seq = (double)longest * std::max(1.0, 0.9 * (double)(q.nseq * q.Hv * vt) / 1024.0);
     const int64_t waves = q.nseq * q.Hv * (vt + kt);
     int64_t G = std::max<int64_t>(1, 4096 / waves);
-    while (G > 2 && G * G > 4 * longest) G = G * 3 / 4;
+    while (G > 2 && G * G > 2 * longest) G = G * 3 / 4;
     if (G < 2) return 0;
     const double seg = 0.9 * (double)total * (double)q.Hv * (1.75 * (double)vt + 0.75 * (double)kt) / 1024.0 + 0.5 * (double)G + 10.0;
     if (seg >= seq) return 0;
