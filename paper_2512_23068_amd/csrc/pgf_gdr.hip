@@ -260,20 +260,19 @@ extern "C" int pgf_gdr_scan(const void *q, const void *k, const void *v, const f
     if (rc != PGF_OK) return rc;
     if (!p->workspace || p->workspace_bytes < pl.total || ((uintptr_t)p->workspace & 255)) return PGF_ERR_WORKSPACE;
     const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;
-    const size_t no = extent(p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e);
+    const Arr out{o, p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e};
     const size_t ns = (size_t)(pl.nseq * pl.Hv * pl.dk * pl.dv) * 4;
-    const struct { const void *p; size_t n; } ins[] = {
-        {q, extent(p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e)}, {k, extent(p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e)},
-        {v, extent(p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {g, extent(p->g_strides, pl.B, pl.Hv, pl.L, 1, 4)},
-        {beta, extent(p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4)}, {p->S_in, ns}};
+    const Arr ins[] = {{q, p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {k, p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
+                       {v, p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {g, p->g_strides, pl.B, pl.Hv, pl.L, 1, 4},
+                       {beta, p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4}};
     for (const auto &i : ins)
-        if (overlaps(o, no, i.p, i.n) || overlaps(p->workspace, pl.total, i.p, i.n)) return PGF_ERR_INVALID_ARG;
+        if (overlaps(out, i) || overlaps(p->workspace, pl.total, i.p, i.bytes()) || overlaps(p->S_out, ns, i.p, i.bytes()))
+            return PGF_ERR_INVALID_ARG;
     // S_out may be S_in: a state is read before its sequence's last step writes it.
-    for (int i = 0; i < 5; ++i)
-        if (overlaps(p->S_out, ns, ins[i].p, ins[i].n)) return PGF_ERR_INVALID_ARG;
     if (overlaps(p->S_out, ns, p->S_in, ns) && p->S_out != p->S_in) return PGF_ERR_INVALID_ARG;
-    if (overlaps(o, no, p->S_out, ns) || overlaps(p->workspace, pl.total, o, no) ||
-        overlaps(p->workspace, pl.total, p->S_out, ns))
+    const size_t no = out.bytes();
+    if (overlaps(o, no, p->S_in, ns) || overlaps(o, no, p->S_out, ns) || overlaps(p->workspace, pl.total, o, no) ||
+        overlaps(p->workspace, pl.total, p->S_in, ns) || overlaps(p->workspace, pl.total, p->S_out, ns))
         return PGF_ERR_INVALID_ARG;
     (void)hipGetLastError();
     Args a = make_args(pl, p, q, k, v, g, beta, o);
@@ -300,15 +299,16 @@ extern "C" int pgf_gdr_step(const void *q, const void *k, const void *v, const f
     if (p->pool && (!p->S_pool || ((uintptr_t)p->S_pool & 15))) return PGF_ERR_INVALID_ARG;
     const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;
     if ((double)p->pool * (double)(pl.Hv * pl.dk * pl.dv) > 1e18) return PGF_ERR_UNSUPPORTED;
-    const size_t no = extent(p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e);
+    const Arr out{o, p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e};
     const size_t ns = (size_t)(p->pool * pl.Hv * pl.dk * pl.dv) * 4;
-    const struct { const void *p; size_t n; } ins[] = {
-        {q, extent(p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e)}, {k, extent(p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e)},
-        {v, extent(p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {g, extent(p->g_strides, pl.B, pl.Hv, pl.L, 1, 4)},
-        {beta, extent(p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4)}, {p->slots, (size_t)pl.B * 4}};
+    const Arr ins[] = {{q, p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {k, p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
+                       {v, p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {g, p->g_strides, pl.B, pl.Hv, pl.L, 1, 4},
+                       {beta, p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4}};
     for (const auto &i : ins)
-        if (overlaps(o, no, i.p, i.n) || overlaps(p->S_pool, ns, i.p, i.n)) return PGF_ERR_INVALID_ARG;
-    if (overlaps(o, no, p->S_pool, ns)) return PGF_ERR_INVALID_ARG;
+        if (overlaps(out, i) || overlaps(p->S_pool, ns, i.p, i.bytes())) return PGF_ERR_INVALID_ARG;
+    const size_t no = out.bytes(), nsl = (size_t)pl.B * 4;
+    if (overlaps(o, no, p->S_pool, ns) || overlaps(o, no, p->slots, nsl) || overlaps(p->S_pool, ns, p->slots, nsl))
+        return PGF_ERR_INVALID_ARG;
     if (pl.L == 0) return PGF_OK;
     (void)hipGetLastError();
     const Args a = make_args(pl, p, q, k, v, g, beta, o);

@@ -762,25 +762,24 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     if (!p->workspace || p->workspace_bytes < pl.total || ((uintptr_t)p->workspace & 255)) return PGF_ERR_WORKSPACE;
     const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;
     const size_t ns = (size_t)(pl.nseq * pl.Hv * pl.dk * pl.dv) * 4, ng = (size_t)(pl.B * pl.Hv * pl.L) * 4;
-    const struct { const void *p; size_t n; } ins[] = {
-        {q, extent(p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e)}, {k, extent(p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e)},
-        {v, extent(p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {g, extent(p->g_strides, pl.B, pl.Hv, pl.L, 1, 4)},
-        {beta, extent(p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4)},
-        {do_, extent(p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {p->S_in, ns}, {p->dS_out, ns}};
-    const struct { const void *p; size_t n; } outs[] = {
-        {dq, extent(p->dq_strides, pl.B, pl.Hk, pl.L, pl.dk, e)}, {dk, extent(p->dk_strides, pl.B, pl.Hk, pl.L, pl.dk, e)},
-        {dv, extent(p->dv_strides, pl.B, pl.Hv, pl.L, pl.dv, e)}, {dg, ng}, {dbeta, ng}, {p->dS_in, ns}};
-    for (const auto &o : outs) {
-        for (const auto &i : ins)
-            if (overlaps(o.p, o.n, i.p, i.n)) return PGF_ERR_INVALID_ARG;
-        if (overlaps(p->workspace, pl.total, o.p, o.n)) return PGF_ERR_INVALID_ARG;
-    }
-    for (const auto &i : ins)
-        if (overlaps(p->workspace, pl.total, i.p, i.n)) return PGF_ERR_INVALID_ARG;
-    // (dq, dk and dv may be parts of one array's rows: only the dense outputs are checked against each other)
-    for (int i = 3; i < 6; ++i)
+    const int64_t dense[3] = {0, 0, 0};
+    const Arr ins[] = {{q, p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {k, p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
+                       {v, p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {do_, p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e},
+                       {g, p->g_strides, pl.B, pl.Hv, pl.L, 1, 4}, {beta, p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4},
+                       {p->S_in, dense, 1, 1, 1, (int64_t)ns, 1}, {p->dS_out, dense, 1, 1, 1, (int64_t)ns, 1}};
+    const Arr outs[] = {{dq, p->dq_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {dk, p->dk_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
+                        {dv, p->dv_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {dg, dense, 1, 1, 1, (int64_t)ng, 1},
+                        {dbeta, dense, 1, 1, 1, (int64_t)ng, 1}, {p->dS_in, dense, 1, 1, 1, (int64_t)ns, 1}};
+    const Arr ws_{p->workspace, dense, 1, 1, 1, (int64_t)pl.total, 1};
+    for (int i = 0; i < 6; ++i) {
+        for (const auto &x : ins)
+            if (overlaps(outs[i], x)) return PGF_ERR_INVALID_ARG;
         for (int j = 0; j < i; ++j)
-            if (overlaps(outs[i].p, outs[i].n, outs[j].p, outs[j].n)) return PGF_ERR_INVALID_ARG;
+            if (overlaps(outs[i], outs[j])) return PGF_ERR_INVALID_ARG;
+        if (overlaps(outs[i], ws_)) return PGF_ERR_INVALID_ARG;
+    }
+    for (const auto &x : ins)
+        if (overlaps(x, ws_)) return PGF_ERR_INVALID_ARG;
     (void)hipGetLastError();
     Args a = make_args(pl, p, q, k, v, g, beta, nullptr);
     a.go = view(do_, p->o_strides, pl.Hv, pl.L, pl.dv);

@@ -59,6 +59,28 @@ bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
     return a && b && na && nb && pa < pb + nb && pb < pa + na;
 }
 
+bool overlaps(const Arr &a, const Arr &b) {
+    if (!overlaps(a.p, a.bytes(), b.p, b.bytes())) return false;
+    int64_t x[3], y[3];
+    dense_strides(a.s, a.H, a.L, a.width, x);
+    dense_strides(b.s, b.H, b.L, b.width, y);
+    if (a.elem != b.elem || a.B != b.B || a.L != b.L) return true;
+    const int64_t e = (int64_t)a.elem, d = (int64_t)((intptr_t)b.p - (intptr_t)a.p);
+    // [0, m) and [d, d + n) repeated every `period` bytes
+    auto apart = [&](int64_t period, int64_t m, int64_t n) {
+        if (period <= 0) return false;
+        const int64_t off = (d % period + period) % period;
+        return off >= m && off + n <= period;
+    };
+    const int64_t hx = (a.H - 1) * x[1] + a.width, hy = (b.H - 1) * y[1] + b.width;      // all heads of a step
+    const bool batches = a.B == 1 || x[0] == y[0];
+    if (a.B > 1 && batches && apart(x[0] * e, (hx + (a.L - 1) * x[2]) * e, (hy + (b.L - 1) * y[2]) * e)) return false;
+    if (a.L > 1 && x[2] == y[2] && batches && (a.B == 1 || (x[2] > 0 && x[0] % x[2] == 0)) &&
+        apart(x[2] * e, hx * e, hy * e))
+        return false;
+    return true;
+}
+
 namespace gdr {
 
 namespace {

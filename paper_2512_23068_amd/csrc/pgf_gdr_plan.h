@@ -61,4 +61,16 @@ void dense_strides(const int64_t (&in)[3], int64_t heads, int64_t L, int64_t wid
 size_t extent(const int64_t (&s)[3], int64_t B, int64_t heads, int64_t L, int64_t width, size_t elem);
 bool overlaps(const void *a, size_t na, const void *b, size_t nb);
 
+// An array of rows as it lies in memory (strides in elements, {0,0,0} dense).
+struct Arr {
+    const void *p;
+    const int64_t (&s)[3];
+    int64_t B, H, L, width;
+    size_t elem;
+    size_t bytes() const { return extent(s, B, H, L, width, elem); }
+};
+// Whether two such arrays share memory.  Arrays whose rows interleave (parts of
+// one fused array: the same batch or step strides, apart within them) do not.
+bool overlaps(const Arr &a, const Arr &b);
+
 }  // namespace pgf

@@ -298,26 +298,23 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
             if (!s.x || !s.y || (grads && !s.dy)) return PGF_ERR_INVALID_ARG;
             if (((uintptr_t)s.x | (uintptr_t)s.y | (grads ? (uintptr_t)s.dy : 0)) & 15) return PGF_ERR_INVALID_ARG;
         }
-        for (const auto &o : sides) {
-            if (!o.H) continue;
-            const size_t ny = extent(o.ys, pl.B, o.H, pl.L, pl.d, e);
-            int64_t oy[3], ix[3];
-            dense_strides(o.ys, o.H, pl.L, pl.d, oy);
-            for (const auto &s : sides) {
-                if (!s.H) continue;
-                // An output over an input: only itself, element on element.
-                const struct { const void *p; const int64_t (&st)[3]; } ins[2] = {{s.x, s.xs}, {grads ? s.dy : nullptr, s.ds}};
-                for (const auto &in : ins) {
-                    if (!overlaps(o.y, ny, in.p, extent(in.st, pl.B, s.H, pl.L, pl.d, e))) continue;
-                    dense_strides(in.st, s.H, pl.L, pl.d, ix);
-                    const bool same = in.p == o.y && &s == &o && ix[0] == oy[0] && ix[1] == oy[1] && ix[2] == oy[2];
-                    // Heads of one fused array: the other side's rows interleave with these.
-                    const bool apart = &s != &o && ix[0] == oy[0] && ix[2] == oy[2];
-                    if (!same && !apart) return PGF_ERR_INVALID_ARG;
-                }
+        const Arr outs[2] = {{qo, p->q_out_strides, pl.B, pl.Hq, pl.L, pl.d, e}, {ko, p->k_out_strides, pl.B, pl.Hk, pl.L, pl.d, e}};
+        const Arr ins[4] = {{q, p->q_strides, pl.B, pl.Hq, pl.L, pl.d, e}, {k, p->k_strides, pl.B, pl.Hk, pl.L, pl.d, e},
+                            {grads ? dq : nullptr, p->dq_strides, pl.B, pl.Hq, pl.L, pl.d, e},
+                            {grads ? dk : nullptr, p->dk_strides, pl.B, pl.Hk, pl.L, pl.d, e}};
+        for (int i = 0; i < 2; ++i) {
+            for (int j = 0; j < 4; ++j) {
+                if (!overlaps(outs[i], ins[j])) continue;
+                // An output over an input: only its own, element on element.
+                int64_t x[3], y[3];
+                dense_strides(outs[i].s, outs[i].H, pl.L, pl.d, x);
+                dense_strides(ins[j].s, ins[j].H, pl.L, pl.d, y);
+                if (j % 2 != i || outs[i].p != ins[j].p || x[0] != y[0] || x[1] != y[1] || x[2] != y[2])
+                    return PGF_ERR_INVALID_ARG;
             }
-            if (overlaps(o.y, ny, p->workspace, pl.total)) return PGF_ERR_INVALID_ARG;
+            if (overlaps(p->workspace, pl.total, outs[i].p, outs[i].bytes())) return PGF_ERR_INVALID_ARG;
         }
+        if (overlaps(outs[0], outs[1])) return PGF_ERR_INVALID_ARG;
     }
     (void)hipGetLastError();
     hipStream_t st = (hipStream_t)stream;
