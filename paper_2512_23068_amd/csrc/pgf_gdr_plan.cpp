@@ -25,7 +25,8 @@ bool strides_ok(const int64_t (&s)[3], int64_t unit, bool out, int64_t B, int64_
         if (s[i] < 0 || s[i] > kMaxStride || s[i] % unit) return false;
         if (out && !dense && L > 0 && n[i] > 1 && !s[i]) return false;
     }
-    return true;
+    // (the array's extent in elements, so that no offset leaves 64 bits)
+    return (double)B * (double)s[0] + (double)H * (double)s[1] + (double)L * (double)s[2] < 1e17;
 }
 
 // Adds a section of n * each bytes; false when the workspace would leave any
