@@ -292,6 +292,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     int64_t n = uni(r.len - r.unit0);
     if (a.seg && n > a.seg) n = a.seg;
     const bool last = r.unit0 + n >= r.len;
+    // Nothing follows the last segment; the adjoint passes through its transition
+    // to all but the first.
+    if (MODE == kSegment && last && (!a.grads || r.unit0 == 0)) return;
     const bool value = tile < a.vt, mine = tile < a.ct;
     const int col = (value ? tile : tile - a.vt) * 16 + c;
     const bool live_col = mine && (value ? col < a.dv : col < a.dk);

@@ -53,6 +53,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int h = (int)(sh - slot * a.Hv), hk = h / a.rep;
     const Rows r = a.seqs.of(slot, a.seg ? a.seg : a.seqs.L + 1, a.seg_per);
     if (r.unit0 > 0 && r.unit0 >= r.len) return;   // uniform over the block
+    if (MODE == kBackSegment && r.unit0 == 0) return;      // (nothing precedes it)
     int64_t n = uni(r.len - r.unit0);
     if (a.seg && n > a.seg) n = a.seg;
     const bool mine = tile < a.vt;
