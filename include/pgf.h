@@ -377,8 +377,8 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
  * Packed sequences: with n_seqs > 0, batch is 1 and the rows of the one
  * batch entry hold n_seqs sequences; sequence n has the rows cu_seqlens[n]
  * <= t < cu_seqlens[n + 1] (device, int32, n_seqs + 1 ascending values in
- * 0 .. L; values outside are clipped).  Rows of no sequence are neither read
- * nor written.  Without it every batch entry is a sequence of L steps.
+ * 0 .. L; values outside are clipped).  Rows of no sequence (before the first,
+ * behind the last) are not read, and not written unless clear_rest is set.  Without it every batch entry is a sequence of L steps.
  *
  * The scan works in chunks of 32 steps: products of the chunk's keys among
  * themselves and with the state on the matrix cores.  bf16 operands enter as
@@ -401,6 +401,8 @@ typedef struct pgf_gdr_params {
     int32_t seg_len;
     float scale;
     int32_t grads;                  /* planning calls: 1 = of pgf_gdr_grads       */
+    int32_t clear_rest;             /* rows of no packed sequence are set to zero in:
+                                       1 every output array, 2 dg and dbeta alone */
     int64_t q_strides[3], k_strides[3], v_strides[3], g_strides[3], beta_strides[3];
     int64_t o_strides[3];           /* o; pgf_gdr_grads: the adjoint signal do_   */
     int64_t dq_strides[3], dk_strides[3], dv_strides[3];

@@ -64,7 +64,7 @@ class PgfGdrParams(ctypes.Structure):
         ("batch", ctypes.c_int64), ("key_heads", ctypes.c_int64), ("value_heads", ctypes.c_int64),
         ("seqlen", ctypes.c_int64), ("d_key", ctypes.c_int64), ("d_value", ctypes.c_int64),
         ("n_seqs", ctypes.c_int64), ("cu_seqlens", _c_f), ("in_dtype", ctypes.c_int32), ("seg_len", ctypes.c_int32),
-        ("scale", ctypes.c_float), ("grads", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("grads", ctypes.c_int32), ("clear_rest", ctypes.c_int32),
         ("q_strides", _i64x3), ("k_strides", _i64x3), ("v_strides", _i64x3), ("g_strides", _i64x3),
         ("beta_strides", _i64x3), ("o_strides", _i64x3), ("dq_strides", _i64x3), ("dk_strides", _i64x3),
         ("dv_strides", _i64x3),
@@ -217,6 +217,8 @@ def _dev_param(v, shape, device, name):
         v = torch.as_tensor(v)
     if tuple(v.shape) != tuple(shape):
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(v.shape)}")
+    if v.dtype is torch.float32 and v.device == device and v.is_contiguous():
+        return v
     return v.to(device=device, dtype=torch.float32).contiguous()
 
 
@@ -674,7 +676,7 @@ def _state(t, shape, dev, name):
 # The parameter structs as struct.pack lays them out (native alignment): one
 # call fills all fields, where a ctypes structure takes one per field; a call's
 # host time is what a single token waits for.
-_GDR_PACK = struct.Struct("@7qPiifi27q5PqPPN")
+_GDR_PACK = struct.Struct("@7qPiifii27q5PqPPN")
 _QK_PACK = struct.Struct("@6qiiif18q4PiqPPPN")
 _NO = (0, 0, 0)
 
@@ -741,10 +743,10 @@ class _Gdr:
         self.n_seqs, self.cu = c.numel() - 1, c.data_ptr()
         self.cell = (self.n_seqs,) + self.cell[1:]
 
-    def pack(self, o, grads=0, out=_NO * 3, states=(0, 0, 0, 0), pool=(0, 0, 0), workspace=None):
+    def pack(self, o, grads=0, out=_NO * 3, states=(0, 0, 0, 0), pool=(0, 0, 0), workspace=None, clear=0):
         ws = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())
         return _GDR_PACK.pack(*self.sizes, self.n_seqs, self.cu, self.dt is torch.bfloat16, self.seg_len, self.scale,
-                              grads, *self.strides, *o, *out, *states, *pool, *ws)
+                              grads, clear, *self.strides, *o, *out, *states, *pool, *ws)
 
     def workspace(self, given, grads=0):
         p = self.pack(_NO, grads)
@@ -781,13 +783,12 @@ def gdr_scan(q, k, v, g, beta, *, scale=None, S_in=None, return_state=False, cu_
         S0 = _state(S_in, c.cell, c.dev, "S_in")
         if out is None:
             o, os = _new_rows(c.v, c.vs)
-            if cu_seqlens is not None:
-                o.zero_()
         else:
             o, os = _rows_out(out, c.v, "out")
         workspace = c.workspace(workspace)
         S_out = torch.empty(c.cell, device=c.dev, dtype=torch.float32) if return_state else None
-        p = c.pack(os, states=(S0, S_out.data_ptr() if return_state else 0, 0, 0), workspace=workspace)
+        p = c.pack(os, states=(S0, S_out.data_ptr() if return_state else 0, 0, 0), workspace=workspace,
+                   clear=out is None)
         _check(lib().pgf_gdr_scan(*c.inputs(), p, o.data_ptr(), _stream_of(c.dev)))
         return (o, S_out) if return_state else o
 
@@ -816,15 +817,13 @@ def gdr_grads(q, k, v, g, beta, do, *, scale=None, S_in=None, dS_out=None, cu_se
                 raise ValueError("out: expected (dq, dk, dv)")
             grads = [_rows_out(t, like, f"out[{i}]") for i, (t, like) in enumerate(zip(out, (c.q, c.k, c.v)))]
         dg, dbeta = (torch.empty(c.g.shape, device=c.dev, dtype=torch.float32) for _ in range(2))
-        if cu_seqlens is not None:
-            for t in ([t for t, _ in grads] if out is None else []) + [dg, dbeta]:
-                t.zero_()
         dS_in = None
         if S_in is not None or dS_out is not None:
             dS_in = torch.empty(c.cell, device=c.dev, dtype=torch.float32)
         workspace = c.workspace(workspace, 1)
         p = c.pack(ds, 1, grads[0][1] + grads[1][1] + grads[2][1],
-                   (S0, 0, dS1, 0 if dS_in is None else dS_in.data_ptr()), workspace=workspace)
+                   (S0, 0, dS1, 0 if dS_in is None else dS_in.data_ptr()), workspace=workspace,
+                   clear=1 if out is None else 2)
         _check(lib().pgf_gdr_grads(*c.inputs(), do.data_ptr(), p, *[t.data_ptr() for t, _ in grads], dg.data_ptr(),
                                    dbeta.data_ptr(), _stream_of(c.dev)))
         return tuple(t for t, _ in grads) + (dg, dbeta) + (() if dS_in is None else (dS_in,))

@@ -282,6 +282,11 @@ extern "C" int pgf_gdr_scan(const void *q, const void *k, const void *v, const f
     a.tr = (float *)(ws + pl.tr);
     hipStream_t st = (hipStream_t)stream;
     const bool bf = p->in_dtype == PGF_BF16;
+    if (p->clear_rest) {
+        Rest rest{};
+        rest.add(a.o, a.Hv, a.dv * (int)e, (int)e);
+        clear_rest(rest, a, st);
+    }
     if (pl.DK == 64) return bf ? scan_t<__bf16, 64>(a, pl, p, st) : scan_t<float, 64>(a, pl, p, st);
     return bf ? scan_t<__bf16, 128>(a, pl, p, st) : scan_t<float, 128>(a, pl, p, st);
 }

@@ -686,5 +686,43 @@ __global__ __launch_bounds__(4 * DK) void k_gdr_carry(Args a) {
     else carry<DK, false>(a, n, h, tile, sS);
 }
 
+// ---------------------------------------------------------------- rows of no sequence
+// Zeroes them (packed sequences follow each other: those before the first and
+// behind the last) in up to five arrays of rows; one block per 64 rows and array.
+struct Rest {
+    View v[5];
+    int H[5], words[5], esize[5];        // heads, 4-byte words of a row, bytes of an element
+    int n = 0;
+    void add(const View &x, int heads, int row_bytes, int es) {
+        v[n] = x;
+        H[n] = heads;
+        words[n] = row_bytes / 4;
+        esize[n++] = es;
+    }
+};
+
+template <typename I>              // (a template only so that both files may hold it)
+__global__ __launch_bounds__(256) void k_gdr_rest(const Rest a, const Seqs seqs) {
+    const int x = blockIdx.y, words = a.words[x];
+    const int64_t lo = seqs.bound(0), hi = seqs.bound(seqs.n);
+    const int64_t t0 = (int64_t)blockIdx.x * 64;
+    const int64_t top = t0 + 64 < seqs.L ? t0 + 64 : seqs.L;
+    if (t0 >= lo && top <= hi) return;
+    const View v = a.v[x];
+    for (int64_t t = t0; t < top; ++t) {
+        if (t >= lo && t < hi) continue;
+        for (int i = threadIdx.x; i < a.H[x] * words; i += 256) {
+            const int h = i / words;
+            *((uint32_t *)((char *)v.p + ((int64_t)h * v.sh + t * v.st) * a.esize[x]) + (i - h * words)) = 0u;
+        }
+    }
+}
+
+inline void clear_rest(const Rest &r, const Args &a, hipStream_t st) {
+    if (!a.seqs.cu || !a.seqs.L) return;
+    hipLaunchKernelGGL((k_gdr_rest<int>), dim3((unsigned)((a.seqs.L + 63) / 64), r.n), dim3(256), 0, st, r,
+                       a.seqs);
+}
+
 }  // namespace gdr
 }  // namespace pgf

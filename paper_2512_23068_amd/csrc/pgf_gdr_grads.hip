@@ -808,6 +808,17 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     a.dbeta = dbeta;
     hipStream_t st = (hipStream_t)stream;
     const bool bf = p->in_dtype == PGF_BF16;
+    if (p->clear_rest) {
+        Rest rest{};
+        if (p->clear_rest == 1) {
+            rest.add(a.dq, a.Hk, a.dk * (int)e, (int)e);
+            rest.add(a.dk_, a.Hk, a.dk * (int)e, (int)e);
+            rest.add(a.dv_, a.Hv, a.dv * (int)e, (int)e);
+        }
+        rest.add(View{dg, 0, pl.L, 1}, a.Hv, 4, 4);
+        rest.add(View{dbeta, 0, pl.L, 1}, a.Hv, 4, 4);
+        clear_rest(rest, a, st);
+    }
     if (pl.DK == 64) return bf ? grads_t<__bf16, 64>(a, pl, st) : grads_t<float, 64>(a, pl, st);
     return bf ? grads_t<__bf16, 128>(a, pl, st) : grads_t<float, 128>(a, pl, st);
 }

@@ -123,6 +123,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     if (q.dk % 8 || q.dk > 128 || q.dv % 8 || q.dv > 4096) return PGF_ERR_UNSUPPORTED;
     if (q.B > kMaxBatch || q.Hv > kMaxHeads || q.L > kMaxLen || p->n_seqs > kMaxBatch) return PGF_ERR_UNSUPPORTED;
     if (p->n_seqs && (q.B != 1 || step)) return PGF_ERR_INVALID_ARG;
+    if (p->clear_rest < 0 || p->clear_rest > 2) return PGF_ERR_INVALID_ARG;
     if (p->seg_len < -1 || (p->seg_len > 0 && p->seg_len % (kSuper * kC))) return PGF_ERR_INVALID_ARG;
     const int64_t unit = p->in_dtype == PGF_BF16 ? 8 : 4;
     const struct { const int64_t (&s)[3]; int64_t unit; bool out; int64_t heads; } arrays[] = {

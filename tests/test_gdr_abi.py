@@ -34,8 +34,9 @@ def test_packed_blocks_are_the_structs():
     for pack, struct in ((binding._GDR_PACK, binding.PgfGdrParams), (binding._QK_PACK, binding.PgfQkParams)):
         assert pack.size == ctypes.sizeof(struct)
     p = binding.PgfGdrParams.from_buffer_copy(binding._GDR_PACK.pack(
-        *range(1, 7), 7, 8, 9, 10, 0.5, 12, *range(100, 127), 13, 14, 15, 16, 17, 18, 19, 20, 21))
-    assert (p.batch, p.d_value, p.n_seqs, p.cu_seqlens, p.in_dtype, p.seg_len, p.scale, p.grads) == (1, 6, 7, 8, 9, 10, 0.5, 12)
+        *range(1, 7), 7, 8, 9, 10, 0.5, 12, 22, *range(100, 127), 13, 14, 15, 16, 17, 18, 19, 20, 21))
+    assert (p.batch, p.d_value, p.n_seqs, p.cu_seqlens, p.in_dtype, p.seg_len, p.scale, p.grads,
+            p.clear_rest) == (1, 6, 7, 8, 9, 10, 0.5, 12, 22)
     assert list(p.q_strides) == [100, 101, 102] and list(p.dv_strides) == [124, 125, 126]
     assert (p.S_in, p.dS_in, p.S_pool, p.pool, p.slots, p.workspace, p.workspace_bytes) == (13, 16, 17, 18, 19, 20, 21)
     p = binding.PgfQkParams.from_buffer_copy(binding._QK_PACK.pack(
@@ -49,6 +50,7 @@ def test_packed_blocks_are_the_structs():
     (dict(), OK), (dict(seqlen=0), OK), (dict(d_key=8, d_value=8), OK), (dict(d_key=128, d_value=4096), OK),
     (dict(batch=0), INVALID), (dict(key_heads=0), INVALID), (dict(value_heads=3), INVALID), (dict(seqlen=-1), INVALID),
     (dict(d_key=0), INVALID), (dict(in_dtype=2), INVALID), (dict(n_seqs=-1), INVALID), (dict(n_seqs=2), INVALID),
+    (dict(clear_rest=2), OK), (dict(clear_rest=3), INVALID), (dict(clear_rest=-1), INVALID),
     (dict(n_seqs=2, batch=1), OK), (dict(seg_len=-2), INVALID), (dict(seg_len=32), INVALID), (dict(seg_len=64), OK),
     (dict(d_key=12), UNSUPPORTED), (dict(d_key=136), UNSUPPORTED), (dict(d_value=4), UNSUPPORTED),
     (dict(d_value=4104), UNSUPPORTED), (dict(batch=1 << 25), UNSUPPORTED), (dict(seqlen=1 << 33), UNSUPPORTED),

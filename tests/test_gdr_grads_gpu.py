@@ -84,7 +84,8 @@ def test_grads_packed(dtype, dk, dv):
     for g in got[:5]:
         assert not g[:, :, :3].any() and not g[:, :, 230:].any()
     out = [torch.full_like(x, 7.0) for x in d[:3]]
-    binding.gdr_grads(*d, dod, cu_seqlens=cud, out=out)
+    got = binding.gdr_grads(*d, dod, cu_seqlens=cud, out=out)
+    assert not any(bool(x[:, :, :3].any() or x[:, :, 230:].any()) for x in got[3:5])
     assert all(bool((x[:, :, :3] == 7).all() and (x[:, :, 230:] == 7).all()) for x in out)
 
 
