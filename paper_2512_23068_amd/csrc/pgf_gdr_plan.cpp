@@ -3,6 +3,7 @@
 #include "pgf_gdr_plan.h"
 
 #include <algorithm>
+#include <cmath>
 
 namespace pgf {
 
@@ -86,29 +87,44 @@ namespace gdr {
 
 namespace {
 
-// Steps per segment, 0 = not cut.  A wave takes 16 columns of one head through a
-// chunk of 32 steps in about 2 us while it has a SIMD to itself, and the GPU
-// (1024 SIMDs) completes one such piece per 1.8 us and SIMD when it is full.
-// Cutting costs the zero-start end states and the transitions (dk more columns,
-// without outputs: 3/4 of the work a column) on top, and the carry, one step of
-// about 1 us after the other.  So the sequences are cut when all that, spread
-// over the GPU, takes less than the longest sequence's chunks in a row; into as
-// many segments as give the first pass about 4 waves a SIMD, fewer where the
-// carry would take longer than a segment.
+// Time in us of a pass of `waves` waves over `chunks` chunks of 32 steps each, on
+// 1024 SIMDs: 2 us a chunk for a wave that has its SIMD to itself, 3 us for two
+// that share one; more follow as those end, half evenly, half in whole rounds.
+double pass(double waves, double chunks) {
+    const double rounds = std::floor(waves / 2048.0), rest = waves - 2048.0 * rounds;
+    const double tail = rest <= 0.0 ? 0.0 : rest <= 1024.0 ? 2.0 : 3.0;
+    if (rounds < 1.0) return chunks * tail;
+    return chunks * 0.5 * (3.0 * rounds + tail + 3.0 * waves / 2048.0);
+}
+
+// Steps per segment, 0 = not cut.  A wave takes 16 columns of one head through
+// its chunks one after the other.  Cutting a sequence costs the zero-start end
+// states and the transitions (dk more columns, without outputs: 3/4 of the work
+// a column) on top, the carry, 2.2 us a segment one after the other, and two more
+// launches.  Of the lengths below, that of the least sum is taken.  Measured, dk =
+// dv = 128, bf16, us for one sequence: 4 heads of 1024 steps 72 uncut, 65 in
+// segments of 256; of 32768 steps 1700 uncut, 422 / 287 / 238 / 277 / 459 in
+// segments of 256 / 512 / 1024 / 2048 / 4096; 32 heads of 16384 steps 952 uncut,
+// 822 / 650 / 599 / 566 / 644.
 int64_t default_seg(const Plan &q, bool packed) {
-    const int64_t vt = cdiv(q.dv, 16), kt = cdiv(q.dk, 16);
-    const int64_t total = cdiv(packed ? q.L : q.B * q.L, kC);
+    const int64_t unit = kSuper * kC, steps = packed ? q.L : q.B * q.L;
     // Packed lengths are on the device: the longest is taken as four times the mean.
-    const int64_t longest = cdiv(packed ? std::min(q.L, 4 * q.L / q.nseq) : q.L, kC);
-    const double seq = (double)longest * std::max(1.0, 0.9 * (double)(q.nseq * q.Hv * vt) / 1024.0);
-    const int64_t waves = q.nseq * q.Hv * (vt + kt);
-    int64_t G = std::max<int64_t>(1, 4096 / waves);
-    while (G > 2 && G * G > 2 * longest) G = G * 3 / 4;
-    if (G < 2) return 0;
-    const double seg = 0.9 * (double)total * (double)q.Hv * (1.75 * (double)vt + 0.75 * (double)kt) / 1024.0 + 0.5 * (double)G + 10.0;
-    if (seg >= seq) return 0;
-    const int64_t unit = kSuper * kC;
-    return std::max<int64_t>(4 * unit, cdiv(cdiv(longest * kC, G), unit) * unit);
+    const int64_t longest = packed ? std::min(q.L, 4 * cdiv(q.L, q.nseq)) : q.L;
+    const double vt = (double)(q.Hv * cdiv(q.dv, 16)), kt = (double)(q.Hv * cdiv(q.dk, 16));
+    double least = std::max(pass((double)q.nseq * vt, (double)cdiv(cdiv(steps, q.nseq), kC)),
+                            (double)cdiv(longest, kC) * 2.0);
+    int64_t seg = 0;
+    for (int64_t n = 4, more = 2; n * unit < longest; n += more) {
+        if (n == 4 * more) more *= 2;
+        const double chunks = (double)(n * unit / kC), pieces = (double)std::max(cdiv(steps, n * unit), q.nseq);
+        const double t = pass(pieces * vt, chunks) + 0.75 * pass(pieces * (vt + kt), chunks) +
+                         2.2 * (double)cdiv(longest, n * unit) + 10.0;
+        if (t < least) {
+            least = t;
+            seg = n * unit;
+        }
+    }
+    return seg;
 }
 
 }  // namespace
