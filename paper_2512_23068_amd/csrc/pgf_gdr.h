@@ -140,16 +140,20 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 // Two f32 as sums of P bf16 numbers each, o[i] the i-th numbers of both: P = 1
 // rounds (error 2^-9 relative), P = 2 leaves 2^-18, P = 3 2^-27 (below an f32's
 // own rounding).  For bf16 inputs P = 1 is exact.  In pairs, as the conversion
-// instruction takes them: 11 instructions for three parts of two numbers.
+// instruction takes them; x - part is the dot product instruction's (-1, 0) . parts
+// + x, exact, so that no part is widened to f32 first: 7 instructions for three
+// parts of two numbers in place of 11.  An infinite number leaves NaN in its
+// neighbour's parts too; neighbours are always summed over together.
 template <int P>
 __device__ __forceinline__ void split2(floatx2 x, bf16x2 (&o)[P]) {
 #pragma unroll
     for (int i = 0; i < P; ++i) {
         o[i] = __builtin_convertvector(x, bf16x2);
         if (i + 1 < P) {
-            const uint32_t u = __builtin_bit_cast(uint32_t, o[i]);
-            x[0] -= __builtin_bit_cast(float, u << 16);
-            x[1] -= __builtin_bit_cast(float, u & 0xffff0000u);
+            uint32_t m0 = 0x0000bf80u, m1 = 0xbf800000u;           // (-1, 0), (0, -1)
+            asm("" : "+s"(m0), "+s"(m1));      // (as immediate operands they are misread)
+            x[0] = __builtin_amdgcn_fdot2_f32_bf16(o[i], __builtin_bit_cast(bf16x2, m0), x[0], false);
+            x[1] = __builtin_amdgcn_fdot2_f32_bf16(o[i], __builtin_bit_cast(bf16x2, m1), x[1], false);
         }
     }
 }
