@@ -245,18 +245,18 @@ __device__ __forceinline__ floatx4 mfma_parts(const Frag<PA> &a, const Frag<PB> 
     return c;
 }
 
-// The same for two row tiles of A, in turn: a product waits for the one before
-// it where both add to the same tile.
-template <int PA, int PB>
-__device__ __forceinline__ void mfma_parts2(const Frag<PA> (&a)[2], const Frag<PB> &b, floatx4 (&c)[2]) {
-    constexpr int N = PA > PB ? PA : PB;
+// The same for N row tiles of A, in turn: a product waits for the one before it
+// where both add to the same tile.
+template <int PA, int PB, int N>
+__device__ __forceinline__ void mfma_parts2(const Frag<PA> (&a)[N], const Frag<PB> &b, floatx4 *c) {
+    constexpr int M = PA > PB ? PA : PB;
 #pragma unroll
-    for (int s = N - 1; s >= 0; --s)
+    for (int s = M - 1; s >= 0; --s)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
             if (s - i >= 0 && s - i < PB) {
-                c[0] = mfma(a[0].p[i], b.p[s - i], c[0]);
-                c[1] = mfma(a[1].p[i], b.p[s - i], c[1]);
+#pragma unroll
+                for (int n = 0; n < N; ++n) c[n] = mfma(a[n].p[i], b.p[s - i], c[n]);
             }
 }
 

@@ -299,53 +299,124 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 }
 
 // ---------------------------------------------------------------- outer
-// A block takes 64 steps of one key head; wave w their tile of 16 steps 16 w ..
-// as columns of every product, and all keys as rows, so that the sums over keys
-// (dbeta, dG) stay in a wave.  Per value head it goes through two sides: side 0
-// has what reads the state (y, S0 dO and the products with earlier steps: dq,
-// r), side 1 what writes it (z and the products with later steps: w).  Phase one
-// of a side runs over the value columns, 32 at a time through LDS in three
-// parts: the products with S0 (or dS1), and the 64 x 64 products of E, dE and
-// dO in the orientation the next product wants them as operand.  Phase two adds
-// the products with K and Q.  One side after the other needs half the registers
-// and LDS of both at once, so that two blocks share a CU and one computes while
-// the other loads.
-// Bound by the matrix cores (2850 instructions a block and head at 128 x 128)
-// and by the reads of S0 and dS1.
+// A block takes 64 steps of one key head; wave w of a side their tile of 16 steps
+// 16 w .. as columns of every product, and all keys as rows, so that the sums over
+// keys (dbeta, dG) stay in a wave.  Four waves are side 0, which has what reads the
+// state (y, S0 dO and the products with earlier steps: dq, r), four side 1, which
+// has what writes it (z and the products with later steps: w); a SIMD holds a wave
+// of each.  Phase one runs over the value columns, 32 at a time through LDS in
+// three parts, which both sides read: the products with S0 (or dS1), and the
+// 64 x 64 products of E, dE and dO in the orientation the next product wants them
+// as operand.  Phase two adds the products with K and Q, and r passes to side 1.
+// At 128 x 128 in bf16 a block takes 94000 cycles, 29000 of them in a
+// SIMD's matrix instructions: the rest is the staging (7 instructions for two numbers' parts)
+// and the waits between the phases, which one block of eight waves a CU (all that
+// the registers hold) does not fill.  1024 blocks of two heads (2 x 4096 steps, 16
+// heads) take 187 us; two blocks of four waves a CU, one side after the other with
+// S0, E and dE read and split twice, took 220 us.
 constexpr int kRun = kC * kSuper;
 constexpr double kLog2e = 1.4426950408889634;
 
 template <typename T, int DK>
 struct OuterLds {
     static constexpr int P = sizeof(T) == 2 ? 1 : 3;
+    struct Cols {
+        __align__(16) char S[2][3][DK * 64];       // S0, dS1: rows of 32 value columns
+        __align__(16) char E[2][3][kRun * 64], dO[P][kRun * 64];       // E and dE
+    };
+    // Two in LDS where they fit: one barrier per 32 columns.
+    static constexpr int NB = 2 * sizeof(Cols) <= 155 * 1024 ? 2 : 1;
     union {
-        struct {
-            __align__(16) char S[3][DK * 64];      // rows of 32 value columns
-            __align__(16) char E[3][kRun * 64], dE[3][kRun * 64], dO[P][kRun * 64];
-        } v;
+        Cols v[NB];
         struct {
             __align__(16) char K[P][kRun * DK * 2], Q[P][kRun * DK * 2];
+            __align__(16) floatx4 r[4 * (DK / 16) * 64];               // [wave][kt][lane]
         } k;
     };
     double G[kRun];                                // sums of g, in powers of two
-    float be[kRun], dG[2][kRun], kz[kRun], dot[4];
+    float be[kRun], dG[2][kRun], kz[kRun], dot[8];
 };
 
-// One side of one value head.  accq, acck: f32 sums on their way over the value
-// heads (and dk's from side to side), in the workspace: each place is written
-// and read by one lane.  In registers they left too few for the products'
-// operands.
+// One side of all value heads of a key head.  accq, acck: f32 sums on their way
+// over the value heads, in the workspace: each place is written and read by one
+// lane.  In registers they left too few for the products' operands.
 template <typename T, int DK, int SIDE>
 __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, const Rows &r, int64_t t0, int live,
-                                           int64_t slot0, int64_t sslot, int hk, int vh, int w, float *accq, float *acck) {
-    constexpr int P = sizeof(T) == 2 ? 1 : 3;
+                                           int64_t slot0, int64_t sslot, int hk, int w, float *accq, float *acck) {
+    using Lds = OuterLds<T, DK>;
+    constexpr int P = Lds::P, NB = Lds::NB;
     constexpr int KT = DK / 16, KU = kRun * DK / 8 / 256;
-    constexpr int SU = DK / 64;                    // 8-column units of S0 (dS1) a thread stages
-    const int h = hk * a.rep + vh, lane = threadIdx.x % 64;
+    // Tiles of 16 rows at a time in the products: two, so that those that add to
+    // the same tile wait less for each other, where their parts leave registers.
+    constexpr int W = P == 1 ? 2 : 1;
+    // The block's 128 rows of threads stage S0 and dS1, one row of each; where a
+    // state has 64 rows side 0 stages S0 and side 1 dS1.
+    constexpr bool S0 = DK == 128 || SIDE == 0, D1 = DK == 128 || SIDE == 1;
+    const int lane = threadIdx.x % 64;
+    int c = lane % 16, qd = lane / 16, tid = threadIdx.x;
+    Raw8<float> r0, r1, re;                        // rows of S0 and dS1, of E (side 0) or dE (side 1)
+    Raw8<T> rg;                                    // of dO (side 1)
+    float gl, bl;                                  // g and beta of step `lane`
+    auto fetch = [&](int vh, int v0) {
+        const int h = hk * a.rep + vh, eu = tid % 4, er = tid % 256 / 4, sr = DK == 128 ? tid / 4 : er;
+        const int64_t cell = (sslot * a.Hv + h) * (int64_t)(a.dk * a.dv);
+        const Buf s0b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveS + cell)), a.dv * 4, a.dk, a.dv * 4);
+        const Buf s1b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveD + cell)), a.dv * 4, a.dk, a.dv * 4);
+        const bool con = v0 + 8 * eu < a.dv;       // this thread's columns are there
+        const uint32_t vc = (uint32_t)(v0 + 8 * eu);
+        const uint32_t at = con ? (uint32_t)sr * (a.dv * 4u) + vc * 4u : kNone;
+        r0 = load8<float>(s0b, at, 0);             // (side 1 for <dS1, S0>)
+        if constexpr (D1) r1 = load8<float>(s1b, at, 0);
+        const int64_t row0 = ((slot0 + (er < live ? er / kC : 0)) * a.Hv + h) * (int64_t)(kC * a.dv) + (er < live ? er % kC * a.dv : 0);
+        const float *ep = (SIDE ? a.saveU : a.saveE) + row0 + (con ? vc : 0);
+        re.x = *(const uintx4 *)ep;
+        re.y = *(const uintx4 *)(ep + 4);
+        if constexpr (SIDE == 1) {
+            const Buf gb = make_buf(row_ptr<T>(a.go, r.b, h, t0), (uint32_t)a.go.st * sizeof(T), live, a.dv * (int)sizeof(T));
+            rg = load8<T>(gb, con ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
+        }
+    };
+    auto gates = [&](int vh) {
+        const int64_t t = t0 + (lane < live ? lane : 0);
+        gl = *a.g.at<const float>(r.b, hk * a.rep + vh, t);
+        bl = *a.beta.at<const float>(r.b, hk * a.rep + vh, t);
+    };
+    float ss = 0.0f;                               // <dS1, S0>
+    auto stage = [&](typename Lds::Cols &v, int v0) {
+        const int eu = tid % 4, er = tid % 256 / 4, sr = DK == 128 ? tid / 4 : er;
+        const uint32_t at = unit_off<32>(er, eu), sat = unit_off<32>(sr, eu);
+        Raw8<float> me = re;
+        if (!(v0 + 8 * eu < a.dv && er < live)) me.x = me.y = uintx4{};
+        const Frag<3> fe = raw_frag<3>(me);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) *(bf16x8 *)&v.E[SIDE][p][at] = fe.p[p];
+        if constexpr (SIDE == 1) {
+            const Frag<P> fg = raw_frag<P>(rg);
+#pragma unroll
+            for (int p = 0; p < P; ++p) *(bf16x8 *)&v.dO[p][at] = fg.p[p];
+        }
+        if constexpr (S0) {
+            const Frag<3> f = raw_frag<3>(r0);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *(bf16x8 *)&v.S[0][p][sat] = f.p[p];
+        }
+        if constexpr (D1) {
+            const Frag<3> f = raw_frag<3>(r1);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) *(bf16x8 *)&v.S[1][p][sat] = f.p[p];
+            const floatx4 a0 = __builtin_bit_cast(floatx4, r0.x), a1 = __builtin_bit_cast(floatx4, r1.x);
+            const floatx4 b0 = __builtin_bit_cast(floatx4, r0.y), b1 = __builtin_bit_cast(floatx4, r1.y);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ss = fmaf(a0[j], a1[j], fmaf(b0[j], b1[j], ss));
+        }
+    };
+    fetch(0, 0);
+    gates(0);
+    for (int vh = 0; vh < a.rep; ++vh) {
+    const int h = hk * a.rep + vh;
     // The lane's place, hidden from the compiler's motion of what does not
     // change out of the loop: the LDS addresses of both phases, kept over the
     // loop, took a hundred registers more than there are.
-    int c = lane % 16, qd = lane / 16, tid = threadIdx.x;
     asm volatile("" : "+v"(c), "+v"(qd), "+v"(tid));
     // ---- phase one
     floatx4 x1[KT], x2[SIDE ? 1 : KT], d1[4], d2[4];      // side 0: y, S0 dO; side 1: z
@@ -356,155 +427,91 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) d1[i] = d2[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-    float ss = 0.0f;                           // <dS1, S0>
-    const int64_t cell = (sslot * a.Hv + h) * (int64_t)(a.dk * a.dv);
-    const Buf s0b = make_buf((const void *)uni((int64_t)(uintptr_t)((SIDE ? a.saveD : a.saveS) + cell)), a.dv * 4, a.dk, a.dv * 4);
-    const Buf s1b = make_buf((const void *)uni((int64_t)(uintptr_t)(a.saveS + cell)), a.dv * 4, a.dk, a.dv * 4);
-    const Buf gb = make_buf(row_ptr<T>(a.go, r.b, h, t0), (uint32_t)a.go.st * sizeof(T), live, a.dv * (int)sizeof(T));
-    const int eu = tid % 4, er = tid / 4;      // unit and row (of S0, E, dE and dO)
-    const bool elive = er < live;
-    const int64_t eat = ((slot0 + (elive ? er / kC : 0)) * a.Hv + h) * (int64_t)(kC * a.dv) + (elive ? er % kC * a.dv : 0);
-    Raw8<float> r0[SU], r1[SIDE ? SU : 1], re, rd;      // (side 1: S0 too, for <dS1, S0>)
-    Raw8<T> rg;
-    auto fetch = [&](int v0) {
-        const bool con = v0 + 8 * eu < a.dv;   // this thread's columns are there
-        const uint32_t vc = (uint32_t)(v0 + 8 * eu);
-#pragma unroll
-        for (int i = 0; i < SU; ++i) {
-            const uint32_t at = con ? (uint32_t)(er + 64 * i) * (a.dv * 4u) + vc * 4u : kNone;
-            r0[i] = load8<float>(s0b, at, 0);
-            if constexpr (SIDE == 1) r1[i] = load8<float>(s1b, at, 0);
-        }
-        const float *ep = a.saveE + eat + (con ? vc : 0), *dp = a.saveU + eat + (con ? vc : 0);
-        re.x = *(const uintx4 *)ep;
-        re.y = *(const uintx4 *)(ep + 4);
-        rd.x = *(const uintx4 *)dp;
-        rd.y = *(const uintx4 *)(dp + 4);
-        rg = load8<T>(gb, con ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
-    };
-    fetch(0);
-    lds_barrier();                             // (the last side's reads)
+    ss = 0.0f;
+    if (vh) lds_barrier();                         // the last head's reads
+    stage(lds.v[0], 0);
     if (SIDE == 0 && w == 3) {
-        float g = 0.0f, be = 0.0f;
-        if (lane < live) {
-            g = *a.g.at<const float>(r.b, h, t0 + lane);
-            be = *a.beta.at<const float>(r.b, h, t0 + lane);
-            g = g < -200.0f ? -200.0f : g;
-        }
-        double G = g;
+        double G = lane < live ? (gl < -200.0f ? -200.0f : gl) : 0.0f;
 #pragma unroll
         for (int m = 1; m < 64; m *= 2) {
             const double o = __shfl_up(G, m, 64);
             if (lane >= m) G += o;
         }
         lds.G[lane] = G * kLog2e;
-        lds.be[lane] = be;
+        lds.be[lane] = lane < live ? bl : 0.0f;
     }
+    const int more = vh + 1 < a.rep ? vh + 1 : vh;
+    fetch(a.dv > 32 ? vh : more, a.dv > 32 ? 32 : 0);
+    lds_barrier();
     for (int v0 = 0; v0 < a.dv; v0 += 32) {
-        if (v0) lds_barrier();                 // the last columns' reads
-        {
-            const uint32_t at = unit_off<32>(er, eu);
-            Raw8<float> me = re, md = rd;
-            if (!(v0 + 8 * eu < a.dv && elive)) {
-                me.x = me.y = uintx4{};
-                md.x = md.y = uintx4{};
-            }
-            const Frag<3> fe = raw_frag<3>(me), fd = raw_frag<3>(md);
-            const Frag<P> fg = raw_frag<P>(rg);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) {
-                *(bf16x8 *)&lds.v.E[p][at] = fe.p[p];
-                *(bf16x8 *)&lds.v.dE[p][at] = fd.p[p];
-            }
-#pragma unroll
-            for (int p = 0; p < P; ++p) *(bf16x8 *)&lds.v.dO[p][at] = fg.p[p];
-#pragma unroll
-            for (int i = 0; i < SU; ++i) {
-                const Frag<3> f = raw_frag<3>(r0[i]);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) *(bf16x8 *)&lds.v.S[p][unit_off<32>(er + 64 * i, eu)] = f.p[p];
-                if constexpr (SIDE == 1) {
-                    const floatx4 a0 = __builtin_bit_cast(floatx4, r0[i].x), a1 = __builtin_bit_cast(floatx4, r1[i].x);
-                    const floatx4 b0 = __builtin_bit_cast(floatx4, r0[i].y), b1 = __builtin_bit_cast(floatx4, r1[i].y);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) ss = fmaf(a0[j], a1[j], fmaf(b0[j], b1[j], ss));
-                }
-            }
-        }
-        fetch(v0 + 32 < a.dv ? v0 + 32 : v0);
-        lds_barrier();
-        // (each operand is read one tile ahead, and no further: more take registers)
+        const typename Lds::Cols &v = lds.v[NB == 2 ? v0 / 32 & 1 : 0];
+        // (operands are read W tiles ahead, and no further: more take registers)
         const uint32_t wa = unit_off<32>(16 * w + c, qd);      // this wave's steps as columns
-        Frag<3> f[2];
-        auto rd_s = [&](int kt) {
+        Frag<3> f[2][W];
+        auto read = [&](int n) {               // rows of S0 (dS1), then of E (dE)
 #pragma unroll
-            for (int p = 0; p < 3; ++p) f[kt & 1].p[p] = *(const bf16x8 *)&lds.v.S[p][unit_off<32>(16 * kt + c, qd)];
+            for (int i = 0; i < W; ++i)
+#pragma unroll
+                for (int p = 0; p < 3; ++p)
+                    f[n & 1][i].p[p] = n < KT / W
+                        ? *(const bf16x8 *)&v.S[SIDE][p][unit_off<32>(16 * (W * n + i) + c, qd)]
+                        : *(const bf16x8 *)&v.E[SIDE][p][unit_off<32>(16 * (W * (n - KT / W) + i) + c, qd)];
         };
         Frag<3> xw;                            // dE or E
         Frag<P> gw;
 #pragma unroll
-        for (int p = 0; p < 3; ++p) xw.p[p] = *(const bf16x8 *)&(SIDE ? lds.v.E : lds.v.dE)[p][wa];
-#pragma unroll
-        for (int p = 0; p < P; ++p) gw.p[p] = *(const bf16x8 *)&lds.v.dO[p][wa];
-        rd_s(0);
+        for (int p = 0; p < 3; ++p) xw.p[p] = *(const bf16x8 *)&v.E[1 - SIDE][p][wa];
         if constexpr (SIDE == 0) {
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                if (kt + 1 < KT) rd_s(kt + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                x1[kt] = mfma_parts<3, 3>(f[kt & 1], xw, x1[kt]);
-                x2[kt] = mfma_parts<3, P>(f[kt & 1], gw, x2[kt]);
+            for (int p = 0; p < P; ++p) gw.p[p] = *(const bf16x8 *)&v.dO[p][wa];
+        }
+        read(0);
+#pragma unroll
+        for (int n = 0; n < (KT + 4) / W; ++n) {
+            if (n + 1 < (KT + 4) / W) read(n + 1);
+            const int i = W * (n - KT / W);
+            Frag<P> fg[W];
+            if (SIDE == 1 && n >= KT / W) {
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+#pragma unroll
+                    for (int p = 0; p < P; ++p) fg[j].p[p] = *(const bf16x8 *)&v.dO[p][unit_off<32>(16 * (i + j) + c, qd)];
             }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                __builtin_amdgcn_sched_barrier(0);
-                Frag<3> fe;
-#pragma unroll
-                for (int p = 0; p < 3; ++p) fe.p[p] = *(const bf16x8 *)&lds.v.E[p][unit_off<32>(16 * i + c, qd)];
-                d1[i] = mfma_parts<3, P>(fe, gw, d1[i]);
-                d2[i] = mfma_parts<3, 3>(fe, xw, d2[i]);
-            }
-        } else {
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                if (kt + 1 < KT) rd_s(kt + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                x1[kt] = mfma_parts<3, 3>(f[kt & 1], xw, x1[kt]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                __builtin_amdgcn_sched_barrier(0);
-                Frag<3> fd;
-                Frag<P> fg;
-                const uint32_t at = unit_off<32>(16 * i + c, qd);
-#pragma unroll
-                for (int p = 0; p < P; ++p) fg.p[p] = *(const bf16x8 *)&lds.v.dO[p][at];
-#pragma unroll
-                for (int p = 0; p < 3; ++p) fd.p[p] = *(const bf16x8 *)&lds.v.dE[p][at];
-                d1[i] = mfma_parts<P, 3>(fg, xw, d1[i]);
-                d2[i] = mfma_parts<3, 3>(fd, xw, d2[i]);
+            __builtin_amdgcn_sched_barrier(0);
+            const Frag<3> (&fp)[W] = f[n & 1];
+            if (n < KT / W) {
+                mfma_parts2<3, 3>(fp, xw, x1 + W * n);
+                if constexpr (SIDE == 0) mfma_parts2<3, P>(fp, gw, x2 + W * n);
+            } else {
+                mfma_parts2<3, 3>(fp, xw, d2 + i);
+                if constexpr (SIDE == 0) mfma_parts2<3, P>(fp, gw, d1 + i);
+                else mfma_parts2<P, 3>(fg, xw, d1 + i);
             }
         }
+        if (v0 + 32 >= a.dv) break;
+        if constexpr (NB == 1) lds_barrier();
+        stage(lds.v[NB == 2 ? (v0 / 32 + 1) & 1 : 0], v0 + 32);
+        const bool on = v0 + 64 < a.dv;        // these columns of this head follow, or the next head's first
+        fetch(on ? vh : more, on ? v0 + 64 : 0);
+        lds_barrier();
     }
+    gates(more);
     // ---- phase two
     asm volatile("" : "+v"(c), "+v"(qd), "+v"(tid));
     const int tok = 16 * w + c;                // this lane's step
-    Raw8<T> rk[KU], rq[KU];
+    const View &kq = SIDE ? a.q : a.k;         // this side stages
+    Raw8<T> rk[KU];
     {
-        const Buf kb = make_buf(row_ptr<T>(a.k, r.b, hk, t0), (uint32_t)a.k.st * sizeof(T), live, a.dk * (int)sizeof(T));
-        const Buf qb = make_buf(row_ptr<T>(a.q, r.b, hk, t0), (uint32_t)a.q.st * sizeof(T), live, a.dk * (int)sizeof(T));
+        const Buf kb = make_buf(row_ptr<T>(kq, r.b, hk, t0), (uint32_t)kq.st * sizeof(T), live, a.dk * (int)sizeof(T));
 #pragma unroll
         for (int i = 0; i < KU; ++i) {
-            const int u = tid + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
+            const int u = tid % 256 + 256 * i, t = u / (DK / 8), e = u % (DK / 8) * 8;
             rk[i] = load8<T>(kb, e < a.dk ? t * kb.st + e * (uint32_t)sizeof(T) : kNone, 0);
-            rq[i] = load8<T>(qb, e < a.dk ? t * qb.st + e * (uint32_t)sizeof(T) : kNone, 0);
         }
     }
-    if constexpr (SIDE == 1) {
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) ss += __shfl_xor(ss, m, 64);
-        if (lane == 0) lds.dot[w] = ss;
-    }
+    for (int m = 1; m < 64; m *= 2) ss += __shfl_xor(ss, m, 64);
+    if (lane == 0) lds.dot[4 * SIDE + w] = ss;
     const double Gt = lds.G[tok], Gend = lds.G[kRun - 1];
     const float be = lds.be[tok];
     // decays and signs of the 64 x 64 products; what has no place is zero
@@ -522,16 +529,19 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
     lds_barrier();                             // phase one's reads
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
-        const int u = tid + 256 * i, t = u / (DK / 8);
+        const int u = tid % 256 + 256 * i, t = u / (DK / 8);
         const uint32_t at = unit_off<DK>(t, u % (DK / 8));
-        const Frag<P> f = raw_frag<P>(rk[i]), x = raw_frag<P>(rq[i]);
+        const Frag<P> f = raw_frag<P>(rk[i]);
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            *(bf16x8 *)&lds.k.K[p][at] = f.p[p];
-            *(bf16x8 *)&lds.k.Q[p][at] = x.p[p];
-        }
+        for (int p = 0; p < P; ++p) *(bf16x8 *)&(SIDE ? lds.k.Q : lds.k.K)[p][at] = f.p[p];
     }
     lds_barrier();
+    // this lane's place in the sums over heads (what is not there, or not yet
+    // written, is some place of them: loads without conditions)
+    auto acc_at = [&](const float *acc, int kt) {
+        const int key = 16 * kt + 4 * qd;
+        return (const floatx4 *)(acc + (vh && key < a.dk ? tok * a.dk + key : 0));
+    };
     // keys 16 kt + 4 qd .. of this lane's step
     auto row4 = [&](const char (*m)[kRun * DK * 2], int kt) {
         floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -565,12 +575,19 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
         for (int b = 0; b < 2; ++b) {
             if (2 * b > w) continue;           // (uniform over the wave)
             const Frag<3> f1 = to_frag<3>(d1[2 * b], d1[2 * b + 1]), f2 = to_frag<3>(d2[2 * b], d2[2 * b + 1]);
+            Frag<P> kf[2][W];
+            auto read = [&](int kt) {
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const Frag<P> kf = tr(lds.k.K, b, kt);
-                if (kt % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-                x2[kt] = mfma_parts<P, 3>(kf, f1, x2[kt]);
-                x1[kt] = mfma_parts<P, 3>(kf, f2, x1[kt]);
+                for (int i = 0; i < W; ++i) kf[kt / W & 1][i] = tr(lds.k.K, b, kt + i);
+            };
+            read(0);
+#pragma unroll
+            for (int kt = 0; kt < KT; kt += W) {
+                const int x = kt / W & 1;
+                if (kt + W < KT) read(kt + W);
+                __builtin_amdgcn_sched_barrier(0);
+                mfma_parts2<P, 3>(kf[x], f1, x2 + kt);
+                mfma_parts2<P, 3>(kf[x], f2, x1 + kt);
             }
         }
 #pragma unroll
@@ -587,15 +604,19 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
 #pragma unroll
         for (int m = 16; m < 64; m *= 2) s += __shfl_xor(s, m, 64);
         if (qd == 0) lds.dG[0][tok] = s;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) lds.k.r[(w * KT + kt) * 64 + lane] = x1[kt];
+        floatx4 sum[KT];                       // of the heads before
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) sum[kt] = *acc_at(accq, kt);
+        lds_barrier();
         T *out = tok < live ? a.dq.at<T>(r.b, hk, t0 + tok) : nullptr;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             const int key = 16 * kt + 4 * qd;
             if (key >= a.dk) continue;
-            floatx4 &aq = *(floatx4 *)(accq + tok * a.dk + key), &ak = *(floatx4 *)(acck + tok * a.dk + key);
-            ak = vh ? ak + x1[kt] : x1[kt];
-            const floatx4 v = vh ? aq + x2[kt] : x2[kt];
-            if (vh + 1 < a.rep) aq = v;
+            const floatx4 v = vh ? sum[kt] + x2[kt] : x2[kt];
+            if (vh + 1 < a.rep) *(floatx4 *)(accq + tok * a.dk + key) = v;
             else if (tok < live) {
                 Raw4<T> x;
 #pragma unroll
@@ -619,11 +640,27 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
         for (int b = 0; b < 2; ++b) {
             if (2 * b + 1 < w) continue;
             const Frag<3> f1 = to_frag<3>(d1[2 * b], d1[2 * b + 1]), f2 = to_frag<3>(d2[2 * b], d2[2 * b + 1]);
+            Frag<P> qf[2][W], kf[2][W];
+            auto read = [&](int kt) {
 #pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                if (kt % 2 == 0) __builtin_amdgcn_sched_barrier(0);
-                x1[kt] = mfma_parts<P, 3>(tr(lds.k.Q, b, kt), f1, x1[kt]);
-                x1[kt] = mfma_parts<P, 3>(tr(lds.k.K, b, kt), f2, x1[kt]);
+                for (int i = 0; i < W; ++i) {
+                    qf[kt / W & 1][i] = tr(lds.k.Q, b, kt + i);
+                    kf[kt / W & 1][i] = tr(lds.k.K, b, kt + i);
+                }
+            };
+            read(0);
+#pragma unroll
+            for (int kt = 0; kt < KT; kt += W) {
+                const int x = kt / W & 1;
+                if (kt + W < KT) read(kt + W);
+                __builtin_amdgcn_sched_barrier(0);
+                floatx4 y[W];
+#pragma unroll
+                for (int i = 0; i < W; ++i) y[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                mfma_parts2<P, 3>(qf[x], f1, x1 + kt);
+                mfma_parts2<P, 3>(kf[x], f2, y);
+#pragma unroll
+                for (int i = 0; i < W; ++i) x1[kt + i] += y[i];
             }
         }
 #pragma unroll
@@ -631,23 +668,6 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
             const floatx4 kx = row4(lds.k.K, kt);
 #pragma unroll
             for (int j = 0; j < 4; ++j) kw = fmaf(kx[j], x1[kt][j], kw);
-        }
-        T *dko = tok < live ? a.dk_.at<T>(r.b, hk, t0 + tok) : nullptr;
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            const int key = 16 * kt + 4 * qd;
-            if (key >= a.dk) continue;
-            floatx4 &ak = *(floatx4 *)(acck + tok * a.dk + key);
-            floatx4 v = ak;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = fmaf(be, x1[kt][j], v[j]);
-            if (vh + 1 < a.rep) ak = v;
-            else if (tok < live) {
-                Raw4<T> x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x.x[j] = (T)v[j];
-                *(Raw4<T> *)(dko + key) = x;
-            }
         }
 #pragma unroll
         for (int m = 16; m < 64; m *= 2) {
@@ -659,7 +679,27 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
             lds.kz[tok] = be * kz;
             if (tok < live) a.dbeta[(r.b * a.Hv + h) * a.seqs.L + t0 + tok] = kw;
         }
+        floatx4 sum[KT];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) sum[kt] = *acc_at(acck, kt);
         lds_barrier();
+        T *dko = tok < live ? a.dk_.at<T>(r.b, hk, t0 + tok) : nullptr;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const int key = 16 * kt + 4 * qd;
+            if (key >= a.dk) continue;
+            floatx4 v = lds.k.r[(w * KT + kt) * 64 + lane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = fmaf(be, x1[kt][j], v[j]);
+            if (vh) v += sum[kt];
+            if (vh + 1 < a.rep) *(floatx4 *)(acck + tok * a.dk + key) = v;
+            else if (tok < live) {
+                Raw4<T> x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x.x[j] = (T)v[j];
+                *(Raw4<T> *)(dko + key) = x;
+            }
+        }
         if (w == vh % 4) {
             double v = (double)lds.dG[0][lane] + lds.dG[1][lane], e = lds.kz[lane];
 #pragma unroll
@@ -668,18 +708,21 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
                 const double x = __shfl_down(v, m, 64);
                 if (lane + m < 64) v += x;
             }
-            const double s01 = (double)lds.dot[0] + lds.dot[1] + lds.dot[2] + lds.dot[3];
+            double s01 = 0.0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s01 += lds.dot[i];
             if (lane < live)
                 a.dg[(r.b * a.Hv + h) * a.seqs.L + t0 + lane] =
                     (float)(v + e + (double)__builtin_amdgcn_exp2f((float)lds.G[kRun - 1]) * s01);
         }
     }
+    }
 }
 
 template <typename T, int DK>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_outer(Args a) {
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_outer(Args a) {
     __shared__ OuterLds<T, DK> lds;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), w = wv % 4;
     const int64_t sslot = blockIdx.x / a.Hk;
     const int hk = (int)(blockIdx.x - sslot * a.Hk);
     const Rows r = a.seqs.of(sslot, kRun, a.save_per);
@@ -689,10 +732,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
 
     float *const accq = a.acc + (sslot * a.Hk + hk) * (int64_t)(2 * kRun * a.dk), *const acck = accq + kRun * a.dk;
-    for (int vh = 0; vh < a.rep; ++vh) {
-        outer_side<T, DK, 0>(a, lds, r, t0, live, slot0, sslot, hk, vh, w, accq, acck);
-        outer_side<T, DK, 1>(a, lds, r, t0, live, slot0, sslot, hk, vh, w, accq, acck);
-    }
+    // (the sides pass the same number of barriers)
+    if (wv < 4) outer_side<T, DK, 0>(a, lds, r, t0, live, slot0, sslot, hk, w, accq, acck);
+    else outer_side<T, DK, 1>(a, lds, r, t0, live, slot0, sslot, hk, w, accq, acck);
 }
 
 // ---------------------------------------------------------------- dispatch
@@ -740,7 +782,7 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
     if (items) {
         Timed tm(3, st);
         const uint32_t n = (uint32_t)(pl.super_slots * pl.Hk);
-        hipLaunchKernelGGL((k_gdr_outer<T, DK>), dim3(n), dim3(256), 0, st, a);
+        hipLaunchKernelGGL((k_gdr_outer<T, DK>), dim3(n), dim3(512), 0, st, a);
     }
     return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;
 }
