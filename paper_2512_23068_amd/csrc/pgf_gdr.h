@@ -305,12 +305,33 @@ struct Seqs {
     }
 };
 
-// A chunk's record (k_gdr_prep), bytes: images of LDS arrays [32][32] of bf16
-// (2 KB each, unit_off<32>, columns in slot order): three parts of TW, PO of TA,
-// then e^G of the 32 steps, and for the gradients three parts of T^.
+// A chunk's record (k_gdr_prep): TW, TA and for the gradients T^, as their tiles
+// (0,0), (1,0), (1,1) of 16 x 16 f32 (1 KB each; what is above them is zero), then
+// e^G of the 32 steps.
+constexpr uint32_t kTile = 1024, kMat = 3 * kTile;
+__host__ __device__ constexpr uint32_t rec_eG(bool grads) { return (grads ? 3 : 2) * kMat; }
+__host__ __device__ constexpr uint32_t rec_bytes(bool grads) { return rec_eG(grads) + 256; }
+// In LDS they are images [32][32] of bf16, one a part (unit_off<32>, columns in
+// slot order).
 constexpr uint32_t kImg = 2048;
-__host__ __device__ constexpr uint32_t rec_rows(int po) { return (3 + po) * kImg; }
-__host__ __device__ constexpr uint32_t rec_bytes(int po, bool grads) { return rec_rows(po) + 256 + (grads ? 3 * kImg : 0); }
+
+// Lane (r, q) = (l / 4, l % 4) holds columns 4 q .. of row r of tile t: P parts of
+// it into images m[0] ..
+template <int P>
+__device__ __forceinline__ void put_tile(char (*m)[kImg], int t, const uintx4 &x) {
+    const int l = threadIdx.x % 64;
+    const uint32_t at = unit_off<32>(l / 4, l % 4) + (t > 0 ? 16 * 64 : 0) + (t > 1 ? 8 : 0);
+    bf16x4 o[P];
+    split4<P>(__builtin_bit_cast(floatx4, x), o);
+#pragma unroll
+    for (int p = 0; p < P; ++p) *(bf16x4 *)&m[p][at] = o[p];
+}
+// Tile (0,1) of N images: zero, once.
+template <int N, int NT>
+__device__ __forceinline__ void zero_tile(char (*m)[kImg], int tid) {
+    const bf16x4 zero = {};
+    for (int i = tid; i < N * 64; i += NT) *(bf16x4 *)&m[i / 64][unit_off<32>(i % 64 / 4, i % 4) + 8] = zero;
+}
 
 }  // namespace gdr
 }  // namespace pgf

@@ -196,7 +196,7 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
         const int64_t items = pl.chunk_slots * pl.Hk;
         if (items) {
             Timed tm(0, st);
-            hipLaunchKernelGGL((k_gdr_prep<T, DK, rec_parts<T>(false)>), dim3((unsigned)((items + kPrepWaves - 1) / kPrepWaves)),
+            hipLaunchKernelGGL((k_gdr_prep<T, DK>), dim3((unsigned)((items + kPrepWaves - 1) / kPrepWaves)),
                                dim3(64 * kPrepWaves), 0, st, a, pl.chunk_slots);
         }
     }

@@ -40,8 +40,8 @@ struct Args {
 // on the f32 matrix cores, as are the products of TA.  A decay below e^-200 a
 // step is zero in f32, as is e^-200, so -inf (forget everything) is taken as
 // -200 and no difference becomes inf - inf.
-// Bound by memory: it reads q and k once and writes the records (10 KB a chunk
-// and head in bf16).
+// Bound by memory: it reads q and k once and writes the records (6 KB a chunk and
+// head; 9 KB with T^).
 constexpr int kPrepWaves = 4;
 
 // Store at a 32-bit offset from a base that is the same for the whole wave.
@@ -52,7 +52,7 @@ __device__ __forceinline__ floatx4 mfma_f32(float a, float b, floatx4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
 }
 
-template <typename T, int DK, int PO>
+template <typename T, int DK>
 __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu(3))) void k_gdr_prep(Args a, int64_t slots) {
     constexpr int P = sizeof(T) == 2 ? 1 : 3, KS = DK / 32;
     struct Lds {
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
             qk[2] = mfma_parts<P, P>(qf[1], kf[1], qk[2]);
         }
     }
-    const uint32_t rb = rec_bytes(PO, a.grads);
+    const uint32_t rb = rec_bytes(a.grads);
     for (int vh = 0; vh < a.rep; ++vh) {
         const int h = hk * a.rep + vh;
         char *rec = (char *)uni((int64_t)(uintptr_t)(a.rec + (slot * a.Hv + h) * (int64_t)rb));
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
         wave_lds();
         s.G[t] = G;                      // (the upper lanes repeat the lower ones)
         s.be[t] = be;
-        put(rec, rec_rows(PO) + 4 * t, expf((float)G));
+        put(rec, rec_eG(a.grads) + 4 * t, expf((float)G));
         wave_lds();
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
@@ -197,31 +197,13 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
         }
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
-            const int bm = i > 0, bn = i > 1, row = 16 * bm + c;
-            const uint32_t at = unit_off<32>(row, qd) + 8 * bn;
+            const int row = 16 * (i > 0) + c;
+            const uint32_t at = i * kTile + (4 * c + qd) * 16;
             const floatx4 tr = *(const floatx4 *)&s.Ti[i][c][4 * qd];
             const float ob = expf((float)(Gend - s.G[row])) * s.be[row];
-            bf16x4 o[3], u[PO];
-            split4<3>(floatx4{tr[0] * ob, tr[1] * ob, tr[2] * ob, tr[3] * ob}, o);
-            split4<PO>(ta[i], u);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) put(rec, p * kImg + at, o[p]);
-#pragma unroll
-            for (int p = 0; p < PO; ++p) put(rec, (3 + p) * kImg + at, u[p]);
-            if (a.grads) {
-                split4<3>(tr, o);
-#pragma unroll
-                for (int p = 0; p < 3; ++p) put(rec, rec_rows(PO) + 256 + p * kImg + at, o[p]);
-            }
-        }
-        // block (0,1)
-        const uint32_t at = unit_off<32>(c, qd) + 8;
-        const bf16x4 zero = {};
-#pragma unroll
-        for (int p = 0; p < 3 + PO; ++p) put(rec, p * kImg + at, zero);
-        if (a.grads) {
-#pragma unroll
-            for (int p = 0; p < 3; ++p) put(rec, rec_rows(PO) + 256 + p * kImg + at, zero);
+            put(rec, at, floatx4{tr[0] * ob, tr[1] * ob, tr[2] * ob, tr[3] * ob});
+            put(rec, kMat + at, ta[i]);
+            if (a.grads) put(rec, 2 * kMat + at, tr);
         }
     }
 }
@@ -239,10 +221,6 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
 //   kSave     for the gradients: E of every chunk and the state entering every
 //             save-th one
 enum Mode { kOut, kSegment, kSave, kBack, kBackSegment };
-
-// Parts of TA in the records: two where its product is only rounded to bf16.
-template <typename T>
-constexpr int rec_parts(bool grads) { return sizeof(T) == 2 && !grads ? 2 : 3; }
 
 template <typename T, int DK, int MODE>
 struct Chunk {
@@ -271,7 +249,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     constexpr int KS = DK / 32 / HS, KT = DK / 16 / HS;    // of this wave's keys
     constexpr int UNITS = 32 * DK / 8;             // 8-key units of K (and of Q)
     constexpr int KU = (UNITS + NT - 1) / NT;      // those a thread stages
-    constexpr int MU = (NI * 128 + NT - 1) / NT;   // 16-byte units of the images
+    constexpr int NM = MODE == kSegment ? 1 : 2, MU = (3 * NM + 3) / 4;    // matrices, and tiles of them a wave stages
     // Two chunks in LDS where a CU still holds two blocks (one barrier a chunk).
     constexpr int NB = sizeof(Ck) <= 40960 ? 2 : 1;
     __shared__ Ck lds[NB];
@@ -353,8 +331,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const uint32_t vo = live_col && value ? 4 * qd * vst + col * (uint32_t)sizeof(T) : kNone;
     const uint32_t oo = live_col ? 4 * qd * ost + col * (uint32_t)sizeof(T) : kNone;
     const uint32_t kst = (uint32_t)a.k.st * sizeof(T), qst = (uint32_t)a.q.st * sizeof(T);
-    const int rp = rec_parts<T>(a.grads);          // (of the record; this kernel stages what it needs)
-    const uint32_t rb = rec_bytes(rp, a.grads);
+    const uint32_t rb = rec_bytes(a.grads);
     uint32_t ko[KU], qo[KU];
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
@@ -380,10 +357,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         const char *rec = a.rec + ((slot0 + ch) * a.Hv + h) * (int64_t)rb;
 #pragma unroll
         for (int i = 0; i < MU; ++i) {
-            const int u = tid + NT * i < NI * 128 ? tid + NT * i : tid % 128;
-            rm[i] = *(const uintx4 *)(rec + (MODE == kSave && u >= 384 ? rec_rows(rp) + 256 - 384 * 16 : 0u) + 16u * u);
+            const int t = wv + 4 * i < 3 * NM ? wv + 4 * i : 0;        // (none: the first again)
+            rm[i] = *(const uintx4 *)(rec + (t + (MODE == kSave && t >= 3 ? 3 : 0)) * kTile + 16u * lane);
         }
-        reG = *(const float *)(rec + rec_rows(rp) + 4 * (tid % 32));
+        reG = *(const float *)(rec + rec_eG(a.grads) + 4 * (tid % 32));
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -405,13 +382,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             }
         }
 #pragma unroll
-        for (int i = 0; i < MU; ++i)
-            if (64 * wv + NT * i < NI * 128) *(uintx4 *)(&s.M[0][0] + 16 * (tid + NT * i)) = rm[i];
+        for (int i = 0; i < MU; ++i) {
+            const int t = wv + 4 * i;
+            if (t < 3) put_tile<3>(s.M, t, rm[i]);
+            else if (t < 3 * NM) put_tile<NM == 1 ? 1 : NI - 3>(s.M + 3, t - 3, rm[i]);
+        }
         if (tid < 32) s.eG[tid] = reG;
     };
 
     if (chunks > 0) {
         fetch(0);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) zero_tile<NI, NT>(lds[i].M, tid);
         stage(lds[0]);
         lds_barrier();
     }

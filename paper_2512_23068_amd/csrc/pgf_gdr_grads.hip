@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     using Ck = Chunk<T, DK, MODE>;
     constexpr int P = Ck::P, NI = 6;
     constexpr int KS = DK / 32, KT = DK / 16;
-    constexpr int KU = 32 * DK / 8 / 256, MU = NI * 128 / 256;
+    constexpr int KU = 32 * DK / 8 / 256, MU = 2;         // units of K, tiles of TW and TA a thread stages
     constexpr int NB = sizeof(Ck) <= 40960 ? 2 : 1;
     __shared__ Ck lds[NB];
     const int tid = threadIdx.x, lane = tid % 64, c = lane % 16, qd = lane / 16;
@@ -103,7 +103,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const uint32_t kst = (uint32_t)a.k.st * sizeof(T), qst = (uint32_t)a.q.st * sizeof(T);
     const uint32_t go = live_col ? 4 * qd * gst + col * (uint32_t)sizeof(T) : kNone;
     const uint32_t vo = live_col ? 4 * qd * vst + col * (uint32_t)sizeof(T) : kNone;
-    const uint32_t rb = rec_bytes(3, true);
+    const uint32_t rb = rec_bytes(true);
     uint32_t ko[KU], qo[KU];
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
@@ -127,8 +127,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
         const char *rec = a.rec + ((slot0 + ch) * a.Hv + h) * (int64_t)rb;
 #pragma unroll
-        for (int i = 0; i < MU; ++i) rm[i] = *(const uintx4 *)(rec + 16u * (tid + 256 * i));
-        reG = *(const float *)(rec + rec_rows(3) + 4 * (tid % 32));
+        for (int i = 0; i < MU; ++i) rm[i] = *(const uintx4 *)(rec + (w + 4 * i < 6 ? w + 4 * i : 0) * kTile + 16u * lane);
+        reG = *(const float *)(rec + rec_eG(true) + 4 * (tid % 32));
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -147,12 +147,17 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             }
         }
 #pragma unroll
-        for (int i = 0; i < MU; ++i) *(uintx4 *)(&s.M[0][0] + 16 * (tid + 256 * i)) = rm[i];
+        for (int i = 0; i < MU; ++i) {
+            const int t = w + 4 * i;
+            if (t < 6) put_tile<3>(s.M + (t < 3 ? 0 : 3), t < 3 ? t : t - 3, rm[i]);
+        }
         if (tid < 32) s.eG[tid] = reG;
     };
 
     if (chunks > 0) {
         fetch(chunks - 1);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) zero_tile<NI, 256>(lds[i].M, tid);
         stage(lds[0]);
         lds_barrier();
     }
@@ -749,7 +754,7 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
     const int64_t items = pl.chunk_slots * pl.Hk;
     if (items) {
         Timed tm(0, st);
-        hipLaunchKernelGGL((k_gdr_prep<T, DK, 3>), dim3((unsigned)((items + kPrepWaves - 1) / kPrepWaves)),
+        hipLaunchKernelGGL((k_gdr_prep<T, DK>), dim3((unsigned)((items + kPrepWaves - 1) / kPrepWaves)),
                            dim3(64 * kPrepWaves), 0, st, a, pl.chunk_slots);
     }
     if (pl.seg) {

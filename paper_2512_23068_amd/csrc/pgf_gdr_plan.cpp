@@ -170,7 +170,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
     q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
     const int64_t cell = q.Hv * q.dk * q.dv * 4, cell_tr = q.Hv * (int64_t)q.DK * q.DK * 4;
-    q.rec_bytes = kImgBytes * (p->in_dtype == PGF_BF16 && !grads ? 5 : 6) + 256 + (grads ? 3 * kImgBytes : 0);
+    q.rec_bytes = kMatBytes * (grads ? 3 : 2) + 256;
     q.supers_per = cdiv(q.L, kSuper * kC);
     q.super_slots = p->n_seqs ? q.L / (kSuper * kC) + p->n_seqs : q.B * q.supers_per;
     const int64_t ns = q.seg ? q.seg_slots : 0, nc = grads ? q.chunk_slots : 0, nu = grads ? q.super_slots : 0;

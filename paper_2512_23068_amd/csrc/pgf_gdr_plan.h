@@ -13,7 +13,7 @@ namespace gdr {
 
 constexpr int kC = 32;           // steps per chunk
 constexpr int kSuper = 2;        // chunks between saved states of the gradients
-constexpr int64_t kImgBytes = 2048;  // a 32 x 32 matrix of bf16
+constexpr int64_t kMatBytes = 3072;  // a chunk's lower triangular matrix: three 16 x 16 tiles of f32
 
 // Workspace sections (bytes, 256-byte aligned).
 //   rec   [chunk slots][Hv]                   k_gdr_prep's record of each chunk
