@@ -53,12 +53,14 @@ __device__ __forceinline__ floatx4 mfma_f32(float a, float b, floatx4 c) {
 }
 
 template <typename T, int DK>
-__global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu(3))) void k_gdr_prep(Args a, int64_t slots) {
+__global__ __launch_bounds__(64 * kPrepWaves)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DK == 128 ? 3 : 4))) void k_gdr_prep(Args a, int64_t slots) {
     constexpr int P = sizeof(T) == 2 ? 1 : 3, KS = DK / 32;
     struct Lds {
-        __align__(16) float D[2][16][20];     // diagonal blocks of N diag(beta), by column
         __align__(16) float L10[16][20];
-        __align__(16) float Ti[3][16][20];     // T^: blocks (0,0), (1,0), (1,1)
+        // T^: blocks (0,0), (1,0), (1,1); the diagonal ones first hold those of
+        // N diag(beta), by column
+        __align__(16) float Ti[3][16][20];
         __align__(16) float A[3][16][20];     // A diag(beta)
         __align__(16) double G[32];
         __align__(16) float be[32];
@@ -147,7 +149,7 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
                 nb[j] = below ? d * kk[i][j] : 0.0f;
                 if (i == 1) s.L10[row][c] = nb[j];
             }
-            if (i != 1) *(floatx4 *)&s.D[bn][c][4 * qd] = nb;
+            if (i != 1) *(floatx4 *)&s.Ti[i][c][4 * qd] = nb;
         }
         wave_lds();
         // column c of diagonal block qd & 1 (the upper lanes repeat the lower
@@ -160,13 +162,14 @@ __global__ __launch_bounds__(64 * kPrepWaves) __attribute__((amdgpu_waves_per_eu
         for (int j = 0; j < 15; ++j) {
 #pragma unroll
             for (int i4 = j / 4 * 4; i4 < 16; i4 += 4) {
-                const floatx4 l = *(const floatx4 *)&s.D[bd][j][i4];
+                const floatx4 l = *(const floatx4 *)&s.Ti[2 * bd][j][i4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (i4 + i > j) tc[i4 + i] = fmaf(-l[i], tc[j], tc[i4 + i]);
             }
             __builtin_amdgcn_sched_barrier(0);     // one column's reads at a time, or all take registers
         }
+        wave_lds();
 #pragma unroll
         for (int i = 0; i < 16; ++i) s.Ti[2 * bd][i][c] = tc[i];
         wave_lds();
