@@ -17,7 +17,7 @@
 //
 // Why chunks of 32: a product with T^ is one contraction of the 16x16x32 matrix
 // instruction, and a chunk's keys, queries, TW and TA take 26 KB of LDS in bf16,
-// so that several blocks share a CU, each with the next chunk behind.
+// so that two blocks share a CU, each with the next chunk behind.
 #include "pgf_gdr_chain.h"
 #include "pgf_timing.h"
 
@@ -29,7 +29,8 @@ namespace gdr {
 // has the keys kg + KG i of the columns 4 cg .. 4 cg + 3.  One pass forms S^T k
 // and S^T q on the decayed state together (o = S^T q + (k.q) u after the
 // write), so a token costs one reduction over the block.  Bound by memory: the
-// state is read and written once, whatever the number of steps.
+// state is read and written once, whatever the number of steps (one step of 4096
+// states of 128 x 128 88 us, 6.0 TB/s); a single state's step by latency (5 us).
 template <typename T, int DK, int CB>
 __global__ __launch_bounds__(256) void k_gdr_step(Args a, float *pool, int64_t n_pool, const int32_t *slots, int64_t L,
                                                   uint32_t n_items) {
@@ -234,9 +235,13 @@ int step_t(const Args &a, const Plan &pl, const pgf_gdr_params *p, hipStream_t s
         hipLaunchKernelGGL((k_gdr_step<T, DK_, CB_>), dim3(xcd_grid(items, (pl.dv + CB_ - 1) / CB_)), dim3(256), 0, st, a, p->S_pool, p->pool,        \
                            p->slots, pl.L, items);                                                                 \
     }
-    // 128 columns a block once these fill the GPU, 32 before (four times the
-    // blocks, each with a quarter of the state).
-    const bool wide = bh * ((pl.dv + 127) / 128) >= 512;
+    // 32 value columns a block for one or two steps: more blocks have loads in
+    // flight (one step of 4096 states of 128 x 128 95 us, with 128 columns a block
+    // 94; of 1024 states 24.8 and 26.7).  Further steps wait for each other within
+    // a block, and a quarter of the blocks wait a quarter of the time once there is
+    // more than the GPU holds (16 steps of 2048 states 247 us, with 128 columns a
+    // block 139; of 256 states 44 and 38, 4 steps of 256 states 16 and 16).
+    const bool wide = pl.L > 2 && bh * ((pl.dv + 127) / 128) >= 256;
     if (pl.DK == 64) {
         if (wide) PGF_STEP(64, 128) else PGF_STEP(64, 32)
     } else {

@@ -41,7 +41,9 @@ struct Args {
 // step is zero in f32, as is e^-200, so -inf (forget everything) is taken as
 // -200 and no difference becomes inf - inf.
 // Bound by memory: it reads q and k once and writes the records (6 KB a chunk and
-// head; 9 KB with T^).
+// head; 9 KB with T^): 0.54 ms for 131072 steps of 32 heads in f32 (3.0 GB), 46 us
+// for 4 x 4096 steps of 16 heads in bf16, where the chain of one head's decays,
+// substitution and products is waited for.
 constexpr int kPrepWaves = 4;
 
 // Store at a 32-bit offset from a base that is the same for the whole wave.
@@ -218,6 +220,12 @@ __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DK == 128 ? 3 : 4))) void k
 // over the rows of the wave's own last result, which lies as the operand it is
 // needed as (see mfma), so nothing crosses waves but the staged chunk; the
 // next one is loaded into registers meanwhile.
+// Bound by issue: at 128 x 128 in bf16 a wave's chunk is 82 matrix instructions of
+// 16 cycles and about 300 vector ones of 2.4, of which half take S and X apart;
+// two waves on a SIMD need 3 us a chunk each, one alone 2 us.  4 x 4096 steps of 16
+// heads take 230 us (of 275 with the records), 131072 steps of 32 heads of 64 x 64
+// in f32 1.1 ms as kOut, there at the memory's rate (5.1 GB).  32 steps a chunk:
+// a longer one has fewer splits of S a step, and longer products with T^.
 //   kOut      outputs, from the true entry state
 //   kSegment  zero-start end state of the segment (value columns) and its
 //             transition (columns of the identity, v = 0)
@@ -237,12 +245,13 @@ struct Chunk {
     __align__(16) float eG[32];
 };
 
-constexpr int64_t kShareWaves = 768;         // waves of column tiles up to which waves share one
 // HS = 2: two waves share a column tile, each with half of the keys; they add
 // their parts of K S and Q S through LDS and both go on from the sum, each
 // updating its keys and writing half the outputs.  A fifth more work for half the
-// chain: taken where one wave a tile leaves SIMDs idle or alone with one wave
-// (which issues only half the instructions two can).
+// chain: taken up to as many tiles as leave every SIMD at most one such wave (16
+// heads of 128 x 128, 2048 steps, us with one wave a tile and with two: 512 tiles
+// 153 and 139, 768 tiles 160 and 188, 1024 tiles 166 and 198).
+constexpr int64_t kShareWaves = 512;
 template <typename T, int DK, int MODE, int HS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_chain(Args a, uint32_t n_items) {
     using Ck = Chunk<T, DK, MODE>;
@@ -576,7 +585,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // (E's place receives the entry state).  BACK: the adjoint leaving each, from
 // the last to the first, with M transposed.  A block has 16 value columns of a
 // head; its four waves share the keys and pass the state's parts through LDS.
-// About 1 us a segment: its products wait for the last segment's.
+// 2.2 us a segment at 128 x 128 (32 segments of 4 heads 69 us): its products wait
+// for the last segment's, and three segments are loaded ahead of them.
 template <int DK, bool BACK>
 __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile, char (*sS)[16 * DK * 2]) {
     constexpr int KS = DK / 32, D = 3;             // segments loaded ahead

@@ -84,7 +84,8 @@ __device__ __forceinline__ void store4(T *p, const floatx4 &v) {
     *(Raw4<T> *)p = r;
 }
 
-// Bound by memory: x is read and y written once (and dy read by the adjoint).
+// Bound by memory: x is read and y written once (and dy read by the adjoint):
+// 16384 steps of 32 heads of 128 in bf16 72 us (3.7 TB/s), the adjoint 99 us (4.1).
 // The next vector is loaded while one is computed, the first ones while the
 // angles are.
 template <typename T, int G, bool GRAD>
