@@ -378,7 +378,8 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
  * batch entry hold n_seqs sequences; sequence n has the rows cu_seqlens[n]
  * <= t < cu_seqlens[n + 1] (device, int32, n_seqs + 1 ascending values in
  * 0 .. L; values outside are clipped).  Rows of no sequence (before the first,
- * behind the last) are not read, and not written unless clear_rest is set.  Without it every batch entry is a sequence of L steps.
+ * behind the last) are not read, and not written unless clear_rest is set.
+ * Without packed sequences every batch entry is a sequence of L steps.
  *
  * The scan works in chunks of 32 steps: products of the chunk's keys among
  * themselves and with the state on the matrix cores.  bf16 operands enter as

@@ -771,7 +771,10 @@ def gdr_scan(q, k, v, g, beta, *, scale=None, S_in=None, return_state=False, cu_
     entry hold that many sequences (a new output is zero in the rows of none;
     a caller's keeps what it held there).
     S_in: entry states [sequences,Hv,dk,dv] float32.  qk_prep: keyword
-    arguments of qk_norm, which then prepares q and k first.
+    arguments of qk_norm, which then prepares q and k first.  seg_len: steps of
+    the segments that sequences are cut into to run side by side (a multiple of
+    64; 0: chosen by the sizes, taking the longest packed sequence as four times
+    the mean; -1: not cut).
     Returns o [B,Hv,L,dv] in q's type, with return_state (o, S_out).
     """
     _on_device("q, k, v, g and beta", q, k, v, g, beta)

@@ -54,6 +54,16 @@ def test_grads(dtype, B, Hk, Hv, L, dk, dv):
     assert all(torch.equal(x, y) for x, y in zip(got, again))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("Hk,Hv,L,dk,dv", [(1, 4, 130, 128, 24), (2, 6, 65, 40, 32), (1, 2, 100, 104, 96), (1, 3, 64, 64, 104)])
+def test_grads_shared_heads(dtype, Hk, Hv, L, dk, dv):
+    """Value heads of one key head follow each other through one to four rounds of 32 value columns."""
+    print(f"case {dtype} {Hk} {Hv} {L} {dk} {dv}", flush=True)
+    c, d = make(1, Hk, Hv, L, dk, dv, dtype, seed=11)
+    do = torch.randn(1, Hv, L, dv, generator=torch.Generator().manual_seed(12)).to(dtype)
+    compare(binding.gdr_grads(*d, do.to(DEV)), reference(c, do, dk ** -0.5), dtype)
+
+
 def test_grads_empty():
     _, d = make(2, 1, 2, 0, 64, 64, F32)
     dS = torch.randn(2, 2, 64, 64, device=DEV)
