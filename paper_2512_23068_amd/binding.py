@@ -613,6 +613,9 @@ def _la_scan_jvp_on(ts, S_in, dS_in, return_state, seg_len, chunk_segs, workspac
     return (o, do) + states
 
 
+_NO = (0, 0, 0)
+
+
 def _bad(t, shape, dev, dtype, name):
     if not (isinstance(t, torch.Tensor) and t.device == dev and t.dtype == dtype):
         raise ValueError(f"{name}: expected a {dtype} tensor on {dev}")
@@ -627,6 +630,8 @@ def _rows(t, shape, dev, dtype, name):
     is copied."""
     if t.dtype is not dtype or t.shape != shape or t.device != dev:
         _bad(t, shape, dev, dtype, name)
+    if t.is_contiguous() and not t.data_ptr() & 15:
+        return t, _NO                  # (dense rows)
     st = t.stride()
     sb, sh, sl = st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else 0, st[2] if shape[2] > 1 else 0
     if len(shape) == 4:
@@ -639,13 +644,15 @@ def _rows(t, shape, dev, dtype, name):
     return t, (sb, sh, sl)
 
 
-def _new_rows(t, strides, dtype=None):
+def _new_rows(t, strides):
     """A new output in the shape and order of t: step-major where t's heads lie
     side by side in each step.  Returns it with its strides."""
+    if strides is _NO:
+        return torch.empty_like(t), _NO
     B, H, L, d = t.shape
     if H > 1 and L > 1 and strides[1] < strides[2]:
         return (torch.empty((B, L, H, d), device=t.device, dtype=t.dtype).transpose(1, 2), (L * H * d, d, H * d))
-    return torch.empty((B, H, L, d), device=t.device, dtype=t.dtype), (H * L * d, L * d, d)
+    return torch.empty_like(t, memory_format=torch.contiguous_format), _NO
 
 
 def _rows_out(t, like, name):
@@ -678,14 +685,16 @@ def _state(t, shape, dev, name):
 # host time is what a single token waits for.
 _GDR_PACK = struct.Struct("@7qPiifii27q5PqPPN")
 _QK_PACK = struct.Struct("@6qiiif18q4PiqPPPN")
-_NO = (0, 0, 0)
+_HERE = contextlib.nullcontext()
+# (without the check for a lazy start: there are device tensors already)
+_device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _on(dev, stream):
     """Context of a call: the tensors' device and the caller's stream, where they
     are not current already."""
-    if stream is None and dev.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
+    if stream is None and dev.index == _device_now():
+        return _HERE
     stack = contextlib.ExitStack()
     stack.enter_context(torch.cuda.device(dev))
     stack.enter_context(_on_stream(stream, dev))
