@@ -138,8 +138,8 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 // Two f32 as sums of P bf16 numbers each, o[i] the i-th numbers of both: P = 1
-// rounds (error 2^-9 relative), P = 2 leaves 2^-18, P = 3 2^-27 (below an f32's
-// own rounding).  For bf16 inputs P = 1 is exact.  In pairs, as the conversion
+// rounds (error 2^-8 relative at most), P = 2 leaves 2^-17, P = 3 nothing (an f32
+// has 24 bits, three times eight).  For bf16 inputs P = 1 is exact.  In pairs, as the conversion
 // instruction takes them; x - part is the dot product instruction's (-1, 0) . parts
 // + x, exact, so that no part is widened to f32 first: 7 instructions for three
 // parts of two numbers in place of 11.  An infinite number leaves NaN in its
@@ -233,7 +233,8 @@ __device__ __forceinline__ bf16x4 read_tr(const void *p) {
 }
 
 // c + A B with A = sum of PA, B = sum of PB numbers; products below the
-// smallest kept part of either are left out (3 and 3 parts: 6 products).
+// smallest kept part of either are left out (3 and 3 parts: 6 products, 2^-24
+// relative to the factors; 2 and 2 parts: 3 products, 2^-15).
 template <int PA, int PB>
 __device__ __forceinline__ floatx4 mfma_parts(const Frag<PA> &a, const Frag<PB> &b, floatx4 c) {
     constexpr int N = PA > PB ? PA : PB;
