@@ -233,6 +233,13 @@ __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DK == 128 ? 3 : 4))) void k
 //             save-th one
 enum Mode { kOut, kSegment, kSave, kBack, kBackSegment };
 
+// Place of M[row][key] in a segment's transition: as the carry's lanes take it, each
+// of their loads 1 KB in a piece.
+template <int DK>
+__device__ __forceinline__ constexpr uint32_t tr_at(int row, int key) {
+    return (uint32_t)((((row / 16 * (DK / 32) + key / 32) * 2 + key % 8 / 4) * 64 + key % 32 / 8 * 16 + row % 16) * 4 + key % 4);
+}
+
 template <typename T, int DK, int MODE>
 struct Chunk {
     static constexpr int P = sizeof(T) == 2 ? 1 : 3;      // parts of q and k
@@ -572,8 +579,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             for (int kt = 0; kt < KT; ++kt)
                 if (key0(kt) < a.dk) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) a.tr[at + (key0(kt) + j) * DK + col] = S[kt][j];
-                    if (a.trT) *(floatx4 *)(a.trT + at + col * DK + key0(kt)) = S[kt];
+                    for (int j = 0; j < 4; ++j) a.tr[at + tr_at<DK>(key0(kt) + j, col)] = S[kt][j];
+                    if (a.trT) *(floatx4 *)(a.trT + at + tr_at<DK>(col, key0(kt))) = S[kt];
                 }
         }
     } else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv, a.dv);
@@ -585,8 +592,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // (E's place receives the entry state).  BACK: the adjoint leaving each, from
 // the last to the first, with M transposed.  A block has 16 value columns of a
 // head; its four waves share the keys and pass the state's parts through LDS.
-// 2.2 us a segment at 128 x 128 (32 segments of 4 heads 69 us): its products wait
-// for the last segment's, and three segments are loaded ahead of them.
+// 1.4 us a segment at 128 x 128 (32 segments of 4 heads 43 us): its products wait
+// for the last segment's, and three segments are loaded ahead of them.  A block
+// reads 64 KB a segment, a thousand cycles of its CU's path to the cache where each
+// load takes whole lines (tr_at); rows as they are took 67 us.
 template <int DK, bool BACK>
 __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile, char (*sS)[16 * DK * 2]) {
     constexpr int KS = DK / 32, D = 3;             // segments loaded ahead
@@ -609,7 +618,7 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
     uint32_t mo[KS];                               // its row of M
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-        mo[ks] = row < a.dk && 32 * ks + 8 * qd < a.dk ? (uint32_t)(row * DK + 32 * ks + 8 * qd) * 4u : kNone;
+        mo[ks] = row < a.dk && 32 * ks + 8 * qd < a.dk ? (uint32_t)((w * KS + ks) * 128 + lane) * 16u : kNone;
     auto state = [&](const float *p) { return Buf{__builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)ebytes, 0x00020000), est}; };
     floatx4 S = {0.0f, 0.0f, 0.0f, 0.0f}, es[D];
     Raw8<float> ms[D][KS];
@@ -620,7 +629,10 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
 #pragma unroll
         for (int j = 0; j < 4; ++j) e[j] = raw_f<float>(load1<float>(eb, so, j * est));
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) m[ks] = load8<float>(mb, mo[ks], 0);
+        for (int ks = 0; ks < KS; ++ks) {
+            m[ks].x = load8<__bf16>(mb, mo[ks], 0).x;
+            m[ks].y = load8<__bf16>(mb, mo[ks], 1024).x;
+        }
     };
     if (init) {
         const Buf ib = state((const float *)uni((int64_t)(uintptr_t)(init + (n * a.Hv + h) * cell)));
@@ -644,18 +656,23 @@ __device__ __forceinline__ void carry(const Args &a, int64_t n, int h, int tile,
         for (int ks = 0; ks < KS; ++ks) mf[ks] = raw_frag<3>(m[ks]);
         fetch(g + D, e, m);
         lds_barrier();
-        Frag<3> sf[KS];
+        Frag<3> sf[2];
+        auto read_s = [&](int ks) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-            for (int p = 0; p < 3; ++p) sf[ks].p[p] = *(const bf16x8 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, 4 * ks + qd)];
+            for (int p = 0; p < 3; ++p) sf[ks & 1].p[p] = *(const bf16x8 *)&buf[p * 16 * DK * 2 + unit_off<DK>(c, 4 * ks + qd)];
+        };
+        read_s(0);
         // two sums in turn: a product waits for the last one of its sum
 #pragma unroll
-        for (int sum = 2; sum >= 0; --sum)
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + 1 < KS) read_s(ks + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            int n = 0;
 #pragma unroll
-            for (int i = 0; i <= sum; ++i)
+            for (int sum = 2; sum >= 0; --sum)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) acc[ks & 1] = mfma(mf[ks].p[i], sf[ks].p[sum - i], acc[ks & 1]);
+                for (int i = 0; i <= sum; ++i, ++n) acc[n & 1] = mfma(mf[ks].p[i], sf[ks & 1].p[sum - i], acc[n & 1]);
+        }
         S = acc[0] + acc[1];
     };
     int g0 = 0;

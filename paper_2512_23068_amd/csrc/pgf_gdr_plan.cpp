@@ -100,12 +100,12 @@ double pass(double waves, double chunks) {
 // Steps per segment, 0 = not cut.  A wave takes 16 columns of one head through
 // its chunks one after the other.  Cutting a sequence costs the zero-start end
 // states and the transitions (dk more columns, without outputs: 3/4 of the work
-// a column) on top, the carry, 2.2 us a segment one after the other, and two more
+// a column) on top, the carry, 1.4 us a segment one after the other, and two more
 // launches.  Of the lengths below, that of the least sum is taken.  Measured, dk =
-// dv = 128, bf16, us for one sequence: 4 heads of 1024 steps 72 uncut, 65 in
-// segments of 256; of 32768 steps 1700 uncut, 422 / 287 / 238 / 277 / 459 in
-// segments of 256 / 512 / 1024 / 2048 / 4096; 32 heads of 16384 steps 952 uncut,
-// 822 / 650 / 599 / 566 / 644.
+// dv = 128, bf16, us for one sequence: 4 heads of 1024 steps 70 uncut, 57 in
+// segments of 256; of 32768 steps 1715 uncut, 334 / 245 / 211 / 257 / 438 in
+// segments of 256 / 512 / 1024 / 2048 / 4096; 32 heads of 16384 steps 928 uncut,
+// 788 / 638 / 556 / 539 / 616.
 int64_t default_seg(const Plan &q, bool packed) {
     const int64_t unit = kSuper * kC, steps = packed ? q.L : q.B * q.L;
     // Packed lengths are on the device: the longest is taken as four times the mean.
@@ -118,7 +118,7 @@ int64_t default_seg(const Plan &q, bool packed) {
         if (n == 4 * more) more *= 2;
         const double chunks = (double)(n * unit / kC), pieces = (double)std::max(cdiv(steps, n * unit), q.nseq);
         const double t = pass(pieces * vt, chunks) + 0.75 * pass(pieces * (vt + kt), chunks) +
-                         2.2 * (double)cdiv(longest, n * unit) + 10.0;
+                         1.4 * (double)cdiv(longest, n * unit) + 10.0;
         if (t < least) {
             least = t;
             seg = n * unit;
