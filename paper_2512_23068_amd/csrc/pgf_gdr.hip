@@ -216,7 +216,7 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
         a.seg_in = a.segE;
     }
     Timed tm(3, st);
-    const int share = pl.seg_slots * pl.Hv * a.ct <= kShareWaves ? 2 : 1;
+    const int share = pl.seg_slots * pl.Hv * a.ct <= kShareTiles ? 2 : 1;
     const int cb = (a.ct + 4 / share - 1) / (4 / share);
     const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * cb);
     const dim3 grid(xcd_grid(items, cb * a.rep));

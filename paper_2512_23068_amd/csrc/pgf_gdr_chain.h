@@ -258,7 +258,6 @@ struct Chunk {
 // chain: taken up to as many tiles as leave every SIMD at most one such wave (16
 // heads of 128 x 128, 2048 steps, us with one wave a tile and with two: 512 tiles
 // 153 and 139, 768 tiles 160 and 188, 1024 tiles 166 and 198).
-constexpr int64_t kShareWaves = 512;
 template <typename T, int DK, int MODE, int HS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_chain(Args a, uint32_t n_items) {
     using Ck = Chunk<T, DK, MODE>;

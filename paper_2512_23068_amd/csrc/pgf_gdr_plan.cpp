@@ -98,27 +98,30 @@ double pass(double waves, double chunks) {
 }
 
 // Steps per segment, 0 = not cut.  A wave takes 16 columns of one head through
-// its chunks one after the other.  Cutting a sequence costs the zero-start end
-// states and the transitions (dk more columns, without outputs: 3/4 of the work
-// a column) on top, the carry, 1.4 us a segment one after the other, and two more
-// launches.  Of the lengths below, that of the least sum is taken.  Measured, dk =
-// dv = 128, bf16, us for one sequence: 4 heads of 1024 steps 70 uncut, 57 in
-// segments of 256; of 32768 steps 1715 uncut, 334 / 245 / 211 / 257 / 438 in
+// its chunks one after the other, two that share a tile in 1.8 us each (the scan's
+// outputs where they are as few as kShareTiles).  Cutting a sequence costs the
+// zero-start end states and the transitions (dk more columns, without outputs: 3/4
+// of the work a column) on top, the carry, 1.4 us a segment one after the other and
+// one block a CU, and two more launches.  Of the lengths below, that of the least
+// sum is taken.  Measured, dk = dv = 128, bf16, us: 4 heads of 1024 steps 70 uncut,
+// 57 in segments of 256; of 32768 steps 1715 uncut, 334 / 245 / 211 / 257 / 438 in
 // segments of 256 / 512 / 1024 / 2048 / 4096; 32 heads of 16384 steps 928 uncut,
-// 788 / 638 / 556 / 539 / 616.
-int64_t default_seg(const Plan &q, bool packed) {
+// 788 / 638 / 556 / 539 / 616; 4 x 16 heads of 4096 steps 261 uncut, 272 in segments
+// of 1024.
+int64_t default_seg(const Plan &q, bool packed, bool grads) {
     const int64_t unit = kSuper * kC, steps = packed ? q.L : q.B * q.L;
     // Packed lengths are on the device: the longest is taken as four times the mean.
     const int64_t longest = packed ? std::min(q.L, 4 * cdiv(q.L, q.nseq)) : q.L;
     const double vt = (double)(q.Hv * cdiv(q.dv, 16)), kt = (double)(q.Hv * cdiv(q.dk, 16));
-    double least = std::max(pass((double)q.nseq * vt, (double)cdiv(cdiv(steps, q.nseq), kC)),
-                            (double)cdiv(longest, kC) * 2.0);
+    const double tiles = (double)q.nseq * vt;
+    double least = std::max(pass(tiles, (double)cdiv(cdiv(steps, q.nseq), kC)), (double)cdiv(longest, kC) * 2.0);
+    if (!grads && tiles <= (double)kShareTiles) least *= 0.9;
     int64_t seg = 0;
     for (int64_t n = 4, more = 2; n * unit < longest; n += more) {
         if (n == 4 * more) more *= 2;
         const double chunks = (double)(n * unit / kC), pieces = (double)std::max(cdiv(steps, n * unit), q.nseq);
         const double t = pass(pieces * vt, chunks) + 0.75 * pass(pieces * (vt + kt), chunks) +
-                         1.4 * (double)cdiv(longest, n * unit) + 10.0;
+                         1.4 * (double)cdiv(longest, n * unit) * std::max(1.0, tiles / 256.0) + 15.0;
         if (t < least) {
             least = t;
             seg = n * unit;
@@ -165,7 +168,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     q.chunk_slots = p->n_seqs ? q.L / kC + p->n_seqs : q.B * q.chunks_per;
     if (q.chunk_slots * q.Hv > kMaxBlocks / col_blocks || q.nseq * q.Hv > kMaxBlocks / col_blocks)
         return PGF_ERR_UNSUPPORTED;
-    q.seg = p->seg_len > 0 ? p->seg_len : p->seg_len < 0 ? 0 : default_seg(q, p->n_seqs > 0);
+    q.seg = p->seg_len > 0 ? p->seg_len : p->seg_len < 0 ? 0 : default_seg(q, p->n_seqs > 0, grads);
     if (q.seg >= q.L) q.seg = 0;
     q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
     q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
