@@ -304,22 +304,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     // S[kt][j]: key key0(kt) + j of this lane's column
     auto key0 = [&](int kt) { return 32 * (hh * KS + kt / 2) + 8 * qd + 4 * (kt & 1); };
     floatx4 S[KT];
+    // States through buffers: lanes and keys without a place read zero and write
+    // nothing, and a lane keeps one offset for all its keys.
+    const uint32_t est = (uint32_t)a.dv * 4, so = live_col ? (uint32_t)((32 * hh * KS + 8 * qd) * a.dv + col) * 4u : kNone;
+    auto state = [&](const float *p) {
+        return Buf{__builtin_amdgcn_make_buffer_rsrc((void *)uni((int64_t)(uintptr_t)p), 0, a.dk * a.dv * 4, 0x00020000), est};
+    };
+    auto place = [&](int kt, int j) { return (uint32_t)(32 * (kt / 2) + 4 * (kt & 1) + j) * est; };
     {
         const float *in = MODE == kSegment ? nullptr : a.seg_in && r.len ? a.seg_in + (slot * a.Hv + h) * a.dk * a.dv
                           : a.S_in ? a.S_in + (r.n * a.Hv + h) * a.dk * a.dv : nullptr;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (in) {                                  // (loads without conditions: a branch around one waits for it)
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const bool on = live_col && key0(kt) < a.dk;       // d_key is a multiple of 8
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    S[kt][j] = *at_off(in, (uint32_t)(on ? (key0(kt) + j) * a.dv + col : 0) * 4u);
-            }
+        if (in) {
+            const Buf ib = state(in);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
-                if (!(live_col && key0(kt) < a.dk)) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[kt][j] = raw_f<float>(load1<float>(ib, so, place(kt, j)));
         }
         if (MODE == kSegment && !value) {
 #pragma unroll
@@ -328,13 +330,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 for (int j = 0; j < 4; ++j) S[kt][j] = key0(kt) + j == col ? 1.0f : 0.0f;
         }
     }
-    auto store_state = [&](float *out, int ld) {
+    auto store_state = [&](float *out) {
+        const Buf ob = state(out);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
-            if (live_col && key0(kt) < a.dk) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) *at_off(out, (uint32_t)((key0(kt) + j) * ld + col) * 4u) = S[kt][j];
-            }
+            for (int j = 0; j < 4; ++j) store1<float>(ob, so, place(kt, j), S[kt][j]);
     };
 
     // What this thread stages of a chunk.  Rows behind the sequence's end read
@@ -418,7 +419,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     for (int ch = 0; ch < chunks; ++ch) {
         if constexpr (MODE == kSave)
             if (mine && ch % a.save == 0)
-                store_state(a.saveS + ((save0 + ch / a.save) * a.Hv + h) * a.dk * a.dv, a.dv);
+                store_state(a.saveS + ((save0 + ch / a.save) * a.Hv + h) * a.dk * a.dv);
         float vv[2][4];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -557,12 +558,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 float *eb = a.saveE + ((slot0 + ch) * a.Hv + h) * (int64_t)(kC * a.dv);
                 floatx4 e[2] = {};
                 mfma_parts2<3, 3>(af, xp, e);
-                if (live_col && hh == 0) {
+                const Buf sb{__builtin_amdgcn_make_buffer_rsrc((void *)uni((int64_t)(uintptr_t)eb), 0, kC * a.dv * 4, 0x00020000), est};
+                const uint32_t eo = live_col ? (uint32_t)(4 * qd * a.dv + col) * 4u : kNone;
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) *at_off(eb, (uint32_t)((16 * m + 4 * qd + j) * a.dv + col) * 4u) = e[m][j];
-                }
+                    for (int j = 0; j < 4; ++j) store1<float>(sb, eo, (16 * m + j) * est, e[m][j]);
             }
         }
         if constexpr (NB == 1) lds_barrier();
@@ -571,7 +572,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
     if (!mine) return;
     if constexpr (MODE == kSegment) {
-        if (value) store_state(a.segE + (slot * a.Hv + h) * a.dk * a.dv, a.dv);
+        if (value) store_state(a.segE + (slot * a.Hv + h) * a.dk * a.dv);
         else if (live_col) {
             const int64_t at = (slot * a.Hv + h) * DK * DK;
 #pragma unroll
@@ -582,7 +583,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                     if (a.trT) *(floatx4 *)(a.trT + at + tr_at<DK>(col, key0(kt))) = S[kt];
                 }
         }
-    } else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv, a.dv);
+    } else if (a.S_out && last) store_state(a.S_out + (r.n * a.Hv + h) * a.dk * a.dv);
 }
 
 // ---------------------------------------------------------------- carry

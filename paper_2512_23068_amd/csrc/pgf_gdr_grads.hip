@@ -66,33 +66,32 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
     const int64_t save0 = uni(a.seqs.slot0(r.n, kC * kSuper, a.save_per) + r.unit0 / (kC * kSuper));
 
-    auto key0 = [&](int kt) { return 32 * (kt / 2) + 8 * qd + 4 * (kt & 1); };
-    floatx4 S[KT];                                 // the adjoint
+    floatx4 S[KT];                                 // the adjoint: key 32 (kt / 2) + 8 qd + 4 (kt % 2) + j
+    const uint32_t est = (uint32_t)a.dv * 4, so = live_col ? (uint32_t)(8 * qd * a.dv + col) * 4u : kNone;
+    const uint32_t eo = live_col ? (uint32_t)(4 * qd * a.dv + col) * 4u : kNone;
+    auto state = [&](const float *p) {
+        return Buf{__builtin_amdgcn_make_buffer_rsrc((void *)uni((int64_t)(uintptr_t)p), 0, a.dk * a.dv * 4, 0x00020000), est};
+    };
+    auto place = [&](int kt, int j) { return (uint32_t)(32 * (kt / 2) + 4 * (kt & 1) + j) * est; };
     {
         const float *in = MODE == kBackSegment ? nullptr : a.dseg_in && r.len ? a.dseg_in + (slot * a.Hv + h) * a.dk * a.dv
                           : a.dS_out ? a.dS_out + (r.n * a.Hv + h) * a.dk * a.dv : nullptr;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
         if (in) {
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt) {
-                const bool on = live_col && key0(kt) < a.dk;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    S[kt][j] = *at_off(in, (uint32_t)(on ? (key0(kt) + j) * a.dv + col : 0) * 4u);
-            }
+            const Buf ib = state(in);
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
-                if (!(live_col && key0(kt) < a.dk)) S[kt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) S[kt][j] = raw_f<float>(load1<float>(ib, so, place(kt, j)));
         }
     }
     auto store_state = [&](float *out) {
+        const Buf ob = state(out);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
-            if (live_col && key0(kt) < a.dk) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) *at_off(out, (uint32_t)((key0(kt) + j) * a.dv + col) * 4u) = S[kt][j];
-            }
+            for (int j = 0; j < 4; ++j) store1<float>(ob, so, place(kt, j), S[kt][j]);
     };
 
     Raw8<T> rk[KU], rq[KU];
@@ -287,13 +286,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) store1<T>(vb, vo, (16 * m + j) * vst, dE[m][j]);
-                if (live_col) {
+                const Buf sb{__builtin_amdgcn_make_buffer_rsrc((void *)uni((int64_t)(uintptr_t)eb), 0, kC * a.dv * 4, 0x00020000), est};
 #pragma unroll
-                    for (int m = 0; m < 2; ++m)
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            *at_off(eb, (uint32_t)((16 * m + 4 * qd + j) * a.dv + col) * 4u) = dE[m][j];
-                }
+                    for (int j = 0; j < 4; ++j) store1<float>(sb, eo, (16 * m + j) * est, dE[m][j]);
             }
         }
         if constexpr (NB == 1) lds_barrier();
