@@ -546,6 +546,26 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
         const int key = 16 * kt + 4 * qd;
         return (const floatx4 *)(acc + (vh && key < a.dk ? tok * a.dk + key : 0));
     };
+    // the sums go on to the next head, or out
+    auto keep = [&](const View &o, float *acc, const floatx4 (&x)[KT]) {
+        if (vh + 1 < a.rep) {
+            const Buf b{__builtin_amdgcn_make_buffer_rsrc((void *)uni((int64_t)(uintptr_t)acc), 0, kRun * a.dk * 4, 0x00020000), 0};
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt) {
+                const uint32_t key = 16 * kt + 4 * qd;
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uintx4, x[kt]), b.r,
+                                                       (int)key < a.dk ? (tok * a.dk + key) * 4u : kNone, 0, 0);
+            }
+            return;
+        }
+        const Buf b = make_buf(row_ptr<T>(o, r.b, hk, t0), (uint32_t)o.st * sizeof(T), live, a.dk * (int)sizeof(T));
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+            const uint32_t key = 16 * kt + 4 * qd, at = (int)key < a.dk && tok < live ? tok * b.st + key * (uint32_t)sizeof(T) : kNone;
+            if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uintx4, x[kt]), b.r, at, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(uintx2, __builtin_convertvector(x[kt], bf16x4)), b.r, at, 0, 0);
+        }
+    };
     // keys 16 kt + 4 qd .. of this lane's step
     auto row4 = [&](const char (*m)[kRun * DK * 2], int kt) {
         floatx4 x = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -614,20 +634,11 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) sum[kt] = *acc_at(accq, kt);
         lds_barrier();
-        T *out = tok < live ? a.dq.at<T>(r.b, hk, t0 + tok) : nullptr;
+        if (vh) {
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-            const int key = 16 * kt + 4 * qd;
-            if (key >= a.dk) continue;
-            const floatx4 v = vh ? sum[kt] + x2[kt] : x2[kt];
-            if (vh + 1 < a.rep) *(floatx4 *)(accq + tok * a.dk + key) = v;
-            else if (tok < live) {
-                Raw4<T> x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x.x[j] = (T)v[j];
-                *(Raw4<T> *)(out + key) = x;
-            }
+            for (int kt = 0; kt < KT; ++kt) x2[kt] += sum[kt];
         }
+        keep(a.dq, accq, x2);
     } else {
         const float out = __builtin_amdgcn_exp2f((float)(Gend - Gt));
         float kz = 0.0f, kw = 0.0f;
@@ -687,23 +698,14 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) sum[kt] = *acc_at(acck, kt);
         lds_barrier();
-        T *dko = tok < live ? a.dk_.at<T>(r.b, hk, t0 + tok) : nullptr;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const int key = 16 * kt + 4 * qd;
-            if (key >= a.dk) continue;
-            floatx4 v = lds.k.r[(w * KT + kt) * 64 + lane];
+            const floatx4 rx = lds.k.r[(w * KT + kt) * 64 + lane];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = fmaf(be, x1[kt][j], v[j]);
-            if (vh) v += sum[kt];
-            if (vh + 1 < a.rep) *(floatx4 *)(acck + tok * a.dk + key) = v;
-            else if (tok < live) {
-                Raw4<T> x;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x.x[j] = (T)v[j];
-                *(Raw4<T> *)(dko + key) = x;
-            }
+            for (int j = 0; j < 4; ++j) x1[kt][j] = fmaf(be, x1[kt][j], rx[j]);
+            if (vh) x1[kt] += sum[kt];
         }
+        keep(a.dk_, acck, x1);
         if (w == vh % 4) {
             double v = (double)lds.dG[0][lane] + lds.dG[1][lane], e = lds.kz[lane];
 #pragma unroll
