@@ -34,7 +34,7 @@ namespace gdr {
 // As k_gdr_chain: a wave owns 16 value columns of the adjoint state of one head.
 // kBackSegment: from zero at the segment's end to its start, nothing written on
 // the way.
-// Bound by issue like it: 2 x 4096 steps of 16 heads, 128 x 128 in bf16, 112 us and
+// Bound by issue like it: 2 x 4096 steps of 16 heads, 128 x 128 in bf16, 85 us and
 // 64 us for kBackSegment (512 steps a segment; the forward chain 70 and 87 us).
 template <typename T, int DK, int MODE>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_back(Args a, uint32_t n_items) {
