@@ -419,7 +419,9 @@ typedef struct pgf_gdr_params {
     int64_t pool;
     const int32_t *slots;
     /* Scratch (device), at least pgf_gdr_workspace_bytes(p), 256-byte aligned.
-     * It grows with the number of steps.  Not used by pgf_gdr_step. */
+     * It grows with the number of steps, holds nothing between calls and serves
+     * one call (or replay of a captured one) at a time.  Not used by
+     * pgf_gdr_step. */
     void *workspace;
     size_t workspace_bytes;
 } pgf_gdr_params;

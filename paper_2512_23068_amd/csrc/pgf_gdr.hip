@@ -150,6 +150,7 @@ __global__ __launch_bounds__(256) void k_gdr_step(Args a, float *pool, int64_t n
 }
 
 // ---------------------------------------------------------------- dispatch
+static_assert(rec_bytes(true) == 3 * kMatBytes + 256 && rec_bytes(false) == 2 * kMatBytes + 256, "the planner's records");
 View view(const void *p, const int64_t (&s)[3], int64_t H, int64_t L, int64_t d) {
     int64_t o[3];
     dense_strides(s, H, L, d, o);

@@ -15,7 +15,7 @@ constexpr int kC = 32;           // steps per chunk
 constexpr int kSuper = 2;        // chunks between saved states of the gradients
 // Column tiles of the scan's outputs up to which two waves share one (k_gdr_chain).
 constexpr int64_t kShareTiles = 512;
-constexpr int64_t kMatBytes = 3072;  // a chunk's lower triangular matrix: three 16 x 16 tiles of f32
+constexpr int64_t kMatBytes = 3 * 1024;  // a chunk's lower triangular matrix: three 16 x 16 tiles of f32
 
 // Workspace sections (bytes, 256-byte aligned).
 //   rec   [chunk slots][Hv]                   k_gdr_prep's record of each chunk

@@ -64,6 +64,24 @@ def test_grads_shared_heads(dtype, Hk, Hv, L, dk, dv):
     compare(binding.gdr_grads(*d, do.to(DEV)), reference(c, do, dk ** -0.5), dtype)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_grads_widest(dtype):
+    """The largest head: 128 keys, 4096 value columns; the scan and the steps of the same."""
+    c, d = make(1, 1, 1, 70, 128, 4096, dtype, seed=13)
+    gen = torch.Generator().manual_seed(14)
+    S0, dS1 = (torch.randn(1, 1, 128, 4096, generator=gen) * 0.5 for _ in range(2))
+    do = torch.randn(1, 1, 70, 4096, generator=gen).to(dtype)
+    got = binding.gdr_grads(*d, do.to(DEV), S_in=S0.to(DEV), dS_out=dS1.to(DEV))
+    compare(got, reference(c, do, 128 ** -0.5, S0, dS1), dtype)
+    want, wS = ref.scan(*c, 128 ** -0.5, S0)
+    o, S = binding.gdr_scan(*d, S_in=S0.to(DEV), return_state=True)
+    check("o", o, want, TOL[dtype])
+    check("S", S, wS, TOL[F32])
+    S = S0.to(DEV)
+    check("o of steps", binding.gdr_step(*d, S), want, TOL[dtype])
+    check("S of steps", S, wS, TOL[F32])
+
+
 def test_grads_empty():
     _, d = make(2, 1, 2, 0, 64, 64, F32)
     dS = torch.randn(2, 2, 64, 64, device=DEV)
