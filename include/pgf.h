@@ -384,9 +384,9 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
  * The scan works in chunks of 32 steps: products of the chunk's keys among
  * themselves and with the state on the matrix cores.  bf16 operands enter as
  * they are, every f32 operand (state, decays, inner results) as a sum of
- * three bf16 numbers (two where the result is rounded to bf16), so sums and
- * states have f32 accuracy.  A value that is not finite may reach the outputs
- * of its own chunk of 32 steps, but no earlier chunk, other sequence or head.
+ * three bf16 numbers, so sums and states have f32 accuracy and a bf16 output is
+ * rounded once.  A value that is not finite may reach the outputs of its own
+ * chunk of 32 steps, but no earlier chunk, other sequence or head.
  * Results do not change from run to run. */
 typedef struct pgf_gdr_params {
     /* Sizes.  batch, key_heads >= 1; value_heads a multiple of key_heads;

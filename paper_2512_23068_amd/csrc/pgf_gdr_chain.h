@@ -220,7 +220,7 @@ __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DK == 128 ? 3 : 4))) void k
 // over the rows of the wave's own last result, which lies as the operand it is
 // needed as (see mfma), so nothing crosses waves but the staged chunk; the
 // next one is loaded into registers meanwhile.
-// Bound by issue: at 128 x 128 in bf16 a wave's chunk is 82 matrix instructions of
+// Bound by issue: at 128 x 128 in bf16 a wave's chunk is 96 matrix instructions of
 // 16 cycles and about 300 vector ones of 2.4, of which half take S and X apart;
 // two waves on a SIMD need 3 us a chunk each, one alone 2 us.  4 x 4096 steps of 16
 // heads take 230 us (of 275 with the records), 131072 steps of 32 heads of 64 x 64
@@ -243,9 +243,8 @@ __device__ __forceinline__ constexpr uint32_t tr_at(int row, int key) {
 template <typename T, int DK, int MODE>
 struct Chunk {
     static constexpr int P = sizeof(T) == 2 ? 1 : 3;      // parts of q and k
-    static constexpr int PO = sizeof(T) == 2 ? 2 : 3;     // parts of f32 operands of the output alone
     static constexpr bool HAS_Q = MODE != kSegment && MODE != kSave;
-    static constexpr int NI = MODE == kOut ? 3 + PO : MODE == kSegment ? 3 : 6;   // images: TW, then TA (kSave: T^)
+    static constexpr int NI = MODE == kSegment ? 3 : 6;   // images: TW, then TA (kSave: T^)
     __align__(16) char K[P][32 * DK * 2];
     __align__(16) char Q[HAS_Q ? P : 1][HAS_Q ? 32 * DK * 2 : 16];
     __align__(16) char M[NI][kImg];
@@ -261,7 +260,7 @@ struct Chunk {
 template <typename T, int DK, int MODE, int HS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_chain(Args a, uint32_t n_items) {
     using Ck = Chunk<T, DK, MODE>;
-    constexpr int P = Ck::P, PO = Ck::PO, NI = Ck::NI;
+    constexpr int P = Ck::P, NI = Ck::NI;
     constexpr bool OUT = MODE == kOut;
     constexpr int NT = 256, TB = 4 / HS;           // threads, column tiles
     constexpr int KS = DK / 32 / HS, KT = DK / 16 / HS;    // of this wave's keys
@@ -404,7 +403,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int i = 0; i < MU; ++i) {
             const int t = wv + 4 * i;
             if (t < 3) put_tile<3>(s.M, t, rm[i]);
-            else if (t < 3 * NM) put_tile<NM == 1 ? 1 : NI - 3>(s.M + 3, t - 3, rm[i]);
+            else if (t < 3 * NM) put_tile<3>(s.M + NI - 3, t - 3, rm[i]);
         }
         if (tid < 32) s.eG[tid] = reG;
     };
@@ -461,11 +460,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 const Frag<3> sp = to_frag<3>(S[2 * ks], S[2 * ks + 1]);
-                Frag<PO> so;
-#pragma unroll
-                for (int p = 0; p < PO; ++p) so.p[p] = sp.p[p];
                 mfma_parts2<P, 3>(kf[ks & 1], sp, kS);
-                if constexpr (OUT) mfma_parts2<P, PO>(qf[ks & 1], so, qS);
+                if constexpr (OUT) mfma_parts2<P, 3>(qf[ks & 1], sp, qS);
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (HS > 1) {
@@ -510,12 +506,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             floatx4 W[2] = {};
             mfma_parts2<3, 3>(tf, xp, W);
             const Frag<3> wp = to_frag<3>(W[0], W[1]);
-            Frag<MODE == kOut ? PO : 3> af[2];
+            Frag<3> af[2];
             if constexpr (MODE != kSegment) {
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int p = 0; p < NI - 3; ++p)
+                    for (int p = 0; p < 3; ++p)
                         af[m].p[p] = *(const bf16x8 *)&s.M[3 + p][unit_off<32>(16 * m + c, qd)];
             }
 #pragma unroll
@@ -538,16 +534,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
                 __builtin_amdgcn_sched_barrier(0);
             }
             if constexpr (OUT) {
-                Frag<PO> xo;
-#pragma unroll
-                for (int p = 0; p < PO; ++p) xo.p[p] = xp.p[p];
                 const Buf ob = make_buf(op + (int64_t)ch * kC * a.o.st, ost, live_rows(ch), a.dv * (int)sizeof(T));
                 if constexpr (HS > 1) {            // (rows 16 hh ..)
-                    const floatx4 o = mfma_parts<PO, PO>(hh ? af[1] : af[0], xo, hh ? qS[1] : qS[0]);
+                    const floatx4 o = mfma_parts<3, 3>(hh ? af[1] : af[0], xp, hh ? qS[1] : qS[0]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) store1<T>(ob, oo, (16 * hh + j) * ost, o[j] * a.scale);
                 } else {
-                    mfma_parts2<PO, PO>(af, xo, qS);
+                    mfma_parts2<3, 3>(af, xp, qS);
 #pragma unroll
                     for (int m = 0; m < 2; ++m)
 #pragma unroll
