@@ -46,7 +46,7 @@ void dense_strides(const int64_t (&in)[3], int64_t heads, int64_t L, int64_t wid
     const bool dense = !in[0] && !in[1] && !in[2];
     out[0] = dense ? heads * L * width : in[0];
     out[1] = dense ? L * width : in[1];
-    out[2] = dense ? width : in[2];
+    out[2] = dense || L <= 1 ? width : in[2];
 }
 
 size_t extent(const int64_t (&s)[3], int64_t B, int64_t heads, int64_t L, int64_t width, size_t elem) {
@@ -152,7 +152,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     for (const auto &a : arrays)
         if (!strides_ok(a.s, a.unit, a.out, q.B, a.heads, q.L)) return PGF_ERR_INVALID_ARG;
     for (const auto &a : arrays)
-        if (a.s[2] * 16 / unit > kMaxStep) return PGF_ERR_UNSUPPORTED;
+        if (q.L > 1 && a.s[2] * 16 / unit > kMaxStep) return PGF_ERR_UNSUPPORTED;
     if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
     q.DK = q.dk <= 64 ? 64 : 128;
     q.nseq = p->n_seqs ? p->n_seqs : q.B;

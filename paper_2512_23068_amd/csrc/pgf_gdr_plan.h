@@ -58,6 +58,8 @@ int make_plan(const pgf_qk_params *p, Plan *q, bool grads);
 }  // namespace qk
 
 // Strides {0,0,0} stand for dense rows of `width` elements in [.., heads, L, width].
+// A single step's row ends with its width, whatever stride its step index has (a
+// slice's, or zero): kernels bound rows by the step stride.
 void dense_strides(const int64_t (&in)[3], int64_t heads, int64_t L, int64_t width, int64_t (&out)[3]);
 // Bytes from the first to behind the last element of such an array (0 if empty).
 size_t extent(const int64_t (&s)[3], int64_t B, int64_t heads, int64_t L, int64_t width, size_t elem);

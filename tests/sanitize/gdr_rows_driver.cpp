@@ -1,0 +1,61 @@
+// The rows of arrays as the kernels of the gated delta rule take them (host
+// planning alone, no device).  The chains write a chunk's 32 rows through a
+// buffer that ends with the last live row, at t * (step stride) for row t: for
+// every output whose strides the planner accepts, the rows behind the last
+// live one lie behind that end.
+//   one     arrays of one step, whatever stride their step index has
+#include <stdio.h>
+#include <string.h>
+
+#include <random>
+
+#include "../../paper_2512_23068_amd/csrc/pgf_gdr_plan.h"
+
+int main(int argc, char **argv) {
+    const bool one = argc > 1 && !strcmp(argv[1], "one");
+    std::mt19937_64 rng(7);
+    auto pick = [&](std::initializer_list<int64_t> v) { return *(v.begin() + rng() % v.size()); };
+    long accepted = 0, failures = 0;
+    for (int i = 0; i < 100000; ++i) {
+        pgf_gdr_params p;
+        memset(&p, 0, sizeof(p));
+        p.batch = pick({1, 2, 3});
+        p.key_heads = pick({1, 2});
+        p.value_heads = p.key_heads * pick({1, 2});
+        p.seqlen = one ? 1 : pick({1, 2, 31, 33, 70});
+        p.d_key = pick({8, 64, 128});
+        p.d_value = pick({8, 40, 64, 200});
+        p.in_dtype = (int)pick({0, 1});
+        p.scale = 1.0f;
+        const int64_t e = p.in_dtype ? 2 : 4;
+        const bool grads = rng() % 2;
+        struct { int64_t (&s)[3]; int64_t heads, width; } outs[] = {
+            {p.o_strides, p.value_heads, p.d_value}, {p.dq_strides, p.key_heads, p.d_key},
+            {p.dk_strides, p.key_heads, p.d_key}, {p.dv_strides, p.value_heads, p.d_value}};
+        for (int k = 0; k < 4; ++k) {
+            if ((k == 0) == grads || rng() % 2) continue;          // (not an output of this call, or dense)
+            auto &o = outs[k];
+            const int64_t w = o.width, n = o.heads;
+            o.s[2] = pick({0, 8, w, n * w, n * w + 64});
+            o.s[1] = pick({w, w * p.seqlen, 8, n > 1 ? w : 0});
+            o.s[0] = pick({n * w * p.seqlen, (n * w + 64) * p.seqlen, p.batch > 1 ? n * w : 0});
+        }
+        pgf::gdr::Plan q;
+        if (pgf::gdr::make_plan(&p, &q, grads, false) != PGF_OK) continue;
+        ++accepted;
+        for (int k = 0; k < 4; ++k) {
+            if ((k == 0) == grads) continue;
+            const auto &o = outs[k];
+            int64_t d[3];
+            pgf::dense_strides(o.s, o.heads, q.L, o.width, d);
+            const int64_t live = (q.L - 1) % 32 + 1, end = ((live - 1) * d[2] + o.width) * e;
+            for (int64_t t = live; t < 32; ++t)
+                if (t * d[2] * e < end) {
+                    ++failures;
+                    break;
+                }
+        }
+    }
+    printf("%ld plans accepted, %ld failures\n", accepted, failures);
+    return accepted > 1000 ? 0 : 1;
+}
