@@ -370,6 +370,8 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
  * key head h / (value_heads / key_heads).  Each of q, k, v, g, beta, o and the
  * gradients has strides in elements for batch, head and step ({0, 0, 0}: dense
  * row-major); the last index is dense.  A stride of zero broadcasts an input.
+ * Rows of outputs lie apart (ordered by stride, each index that moves steps over
+ * all that the ones before it span).
  * q, k, v, o and their gradients are f32 or bf16 (in_dtype); the arrays'
  * addresses and strides are multiples of 16 bytes (g and beta: of 4), a step's
  * stride below 2^24 bytes.

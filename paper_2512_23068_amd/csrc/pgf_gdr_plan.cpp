@@ -18,16 +18,24 @@ constexpr size_t kMaxTotal = size_t(1) << 46;
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Strides of an array of rows of `width` elements: not negative, bounded, in
-// units of 16 bytes; an output's rows must not fall on each other.
-bool strides_ok(const int64_t (&s)[3], int64_t unit, bool out, int64_t B, int64_t H, int64_t L) {
+// units of 16 bytes.  An output's rows lie apart: of the indexes that move, in the
+// order of their strides, each steps over all that the ones before it span.
+bool strides_ok(const int64_t (&s)[3], int64_t unit, bool out, int64_t B, int64_t H, int64_t L, int64_t width) {
     const int64_t n[3] = {B, H, L};
-    const bool dense = !s[0] && !s[1] && !s[2];
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 3; ++i)
         if (s[i] < 0 || s[i] > kMaxStride || s[i] % unit) return false;
-        if (out && !dense && L > 0 && n[i] > 1 && !s[i]) return false;
-    }
     // (the array's extent in elements, so that no offset leaves 64 bits)
-    return (double)B * (double)s[0] + (double)H * (double)s[1] + (double)L * (double)s[2] < 1e17;
+    if ((double)B * (double)s[0] + (double)H * (double)s[1] + (double)L * (double)s[2] >= 1e17) return false;
+    if (!out || L < 1 || (!s[0] && !s[1] && !s[2])) return true;
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int x, int y) { return s[x] < s[y]; });
+    int64_t span = width;
+    for (int i : order) {
+        if (n[i] <= 1) continue;
+        if (s[i] < span) return false;
+        span += (n[i] - 1) * s[i];
+    }
+    return true;
 }
 
 // Adds a section of n * each bytes; false when the workspace would leave any
@@ -145,12 +153,14 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     if (p->clear_rest < 0 || p->clear_rest > 2) return PGF_ERR_INVALID_ARG;
     if (p->seg_len < -1 || (p->seg_len > 0 && p->seg_len % (kSuper * kC))) return PGF_ERR_INVALID_ARG;
     const int64_t unit = p->in_dtype == PGF_BF16 ? 8 : 4;
-    const struct { const int64_t (&s)[3]; int64_t unit; bool out; int64_t heads; } arrays[] = {
-        {p->q_strides, unit, false, q.Hk}, {p->k_strides, unit, false, q.Hk}, {p->v_strides, unit, false, q.Hv},
-        {p->g_strides, 1, false, q.Hv}, {p->beta_strides, 1, false, q.Hv}, {p->o_strides, unit, !grads, q.Hv},
-        {p->dq_strides, unit, grads, q.Hk}, {p->dk_strides, unit, grads, q.Hk}, {p->dv_strides, unit, grads, q.Hv}};
+    const struct { const int64_t (&s)[3]; int64_t unit; bool out; int64_t heads, width; } arrays[] = {
+        {p->q_strides, unit, false, q.Hk, q.dk}, {p->k_strides, unit, false, q.Hk, q.dk},
+        {p->v_strides, unit, false, q.Hv, q.dv}, {p->g_strides, 1, false, q.Hv, 1},
+        {p->beta_strides, 1, false, q.Hv, 1}, {p->o_strides, unit, !grads, q.Hv, q.dv},
+        {p->dq_strides, unit, grads, q.Hk, q.dk}, {p->dk_strides, unit, grads, q.Hk, q.dk},
+        {p->dv_strides, unit, grads, q.Hv, q.dv}};
     for (const auto &a : arrays)
-        if (!strides_ok(a.s, a.unit, a.out, q.B, a.heads, q.L)) return PGF_ERR_INVALID_ARG;
+        if (!strides_ok(a.s, a.unit, a.out, q.B, a.heads, q.L, a.width)) return PGF_ERR_INVALID_ARG;
     for (const auto &a : arrays)
         if (q.L > 1 && a.s[2] * 16 / unit > kMaxStep) return PGF_ERR_UNSUPPORTED;
     if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
@@ -212,7 +222,7 @@ int make_plan(const pgf_qk_params *p, Plan *out, bool grads) {
         {p->q_strides, false, q.Hq}, {p->k_strides, false, q.Hk}, {p->q_out_strides, true, q.Hq},
         {p->k_out_strides, true, q.Hk}, {p->dq_strides, false, q.Hq}, {p->dk_strides, false, q.Hk}};
     for (const auto &a : arrays)
-        if (!strides_ok(a.s, unit, a.out, q.B, a.heads, q.L)) return PGF_ERR_INVALID_ARG;
+        if (!strides_ok(a.s, unit, a.out, q.B, a.heads, q.L, q.d)) return PGF_ERR_INVALID_ARG;
     if ((double)q.B * (double)(q.Hq + q.Hk) * (double)q.L * (double)q.d > 4e18) return PGF_ERR_UNSUPPORTED;
     if ((double)q.B * (double)q.L > (double)kMaxBlocks) return PGF_ERR_UNSUPPORTED;
     q.G = 1;

@@ -4,10 +4,13 @@
 // every output whose strides the planner accepts, the rows behind the last
 // live one lie behind that end.
 //   one     arrays of one step, whatever stride their step index has
+//   apart   arrays of any length; and no two rows of an accepted output share an
+//           element
 #include <stdio.h>
 #include <string.h>
 
 #include <random>
+#include <set>
 
 #include "../../paper_2512_23068_amd/csrc/pgf_gdr_plan.h"
 
@@ -56,6 +59,41 @@ int main(int argc, char **argv) {
                 }
         }
     }
+    // rows of outputs against their elements themselves; rows in whatever order,
+    // as long as the longer strides step over what the shorter ones span, are taken
+    long nested = 0;
+    for (int i = 0; i < 20000 && !one; ++i) {
+        pgf_gdr_params p;
+        memset(&p, 0, sizeof(p));
+        p.batch = pick({1, 2, 3});
+        p.key_heads = p.value_heads = pick({1, 2, 3});
+        p.seqlen = pick({1, 2, 5});
+        p.d_key = p.d_value = 8;
+        p.in_dtype = 1;
+        const int64_t n[3] = {p.batch, p.value_heads, p.seqlen};
+        int order[3] = {0, 1, 2};
+        for (int k = 2; k > 0; --k) std::swap(order[k], order[rng() % (k + 1)]);
+        int64_t span = 8;
+        for (int k : order) {
+            p.o_strides[k] = span + pick({0, 0, 8, 16});
+            span = (n[k] - 1) * p.o_strides[k] + span;
+            span = (span + 7) / 8 * 8;
+        }
+        bool clash = false;
+        const bool change = rng() % 2;
+        if (change) p.o_strides[rng() % 3] = pick({8, 16, 24, 32, 48});
+        std::set<int64_t> seen;
+        for (int64_t b = 0; b < n[0]; ++b)
+            for (int64_t h = 0; h < n[1]; ++h)
+                for (int64_t t = 0; t < n[2]; ++t)
+                    for (int64_t x = 0; x < 8; ++x)
+                        clash |= !seen.insert(b * p.o_strides[0] + h * p.o_strides[1] + t * p.o_strides[2] + x).second;
+        pgf::gdr::Plan q;
+        const bool ok = pgf::gdr::make_plan(&p, &q, false, false) == PGF_OK;
+        if ((ok && clash) || (!ok && !change)) ++failures;
+        nested += ok;
+    }
+    if (!one && nested < 1000) ++failures;
     printf("%ld plans accepted, %ld failures\n", accepted, failures);
     return accepted > 1000 ? 0 : 1;
 }

@@ -1,0 +1,33 @@
+"""Strides, overlaps and sizes of the gated delta rule and the query/key preparation
+that the host takes or refuses (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from paper_2512_23068_amd import binding
+from tests.test_gdr_abi import A, GB, INVALID, OK, gdr, plan, qk
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(), OK), (dict(o_strides=(6400 * 4, 6400, 64)), OK),                   # [B, H, L, d]
+    (dict(o_strides=(64 * 4 * 100, 64, 64 * 4)), OK),                           # [B, L, H, d]
+    (dict(o_strides=(64 * 4, 64, 64 * 8)), OK),                                 # [L, B, H, d]
+    (dict(o_strides=(51200, 72, 512)), OK),                                     # padded rows
+    (dict(o_strides=(25600, 72, 512)), INVALID),                                # (99 steps of 512 reach beyond 25600)
+    (dict(o_strides=(25600, 6400, 56)), INVALID), (dict(o_strides=(25600, 6400, 8)), INVALID),       # rows over each other
+    (dict(o_strides=(25600, 32, 256)), INVALID), (dict(o_strides=(25600, 64, 200)), INVALID),        # heads over steps
+    (dict(o_strides=(6400, 6400, 64)), INVALID), (dict(o_strides=(512, 64, 256)), INVALID),          # batch entries
+    (dict(batch=1, o_strides=(8, 6400, 64)), OK), (dict(seqlen=1, o_strides=(256, 64, 8)), OK),      # (do not move)
+    (dict(v_strides=(25600, 6400, 8), q_strides=(0, 0, 8)), OK)])               # inputs may
+def test_rows_of_outputs(kw, code):
+    assert plan(gdr(**kw))[0] == code
+    if "o_strides" in kw:
+        p = gdr(grads=1, dv_strides=kw["o_strides"], **{n: x for n, x in kw.items() if n != "o_strides"})
+        assert plan(p)[0] == code
+
+
+@pytest.mark.parametrize("strides", [(2560, 640, 56), (2560, 32, 256), (512, 64, 256)])
+def test_rows_of_prepared_queries(strides):
+    good = [A + i * GB for i in range(4)]
+    p = qk(q_out_strides=strides)
+    assert binding.lib().pgf_qk_norm(good[0], good[1], ctypes.byref(p), good[2], good[3], None) == INVALID

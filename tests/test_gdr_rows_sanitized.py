@@ -29,3 +29,8 @@ def run(driver, what):
 def test_rows_of_one_step(driver):
     """A single step's rows end behind it, also where its step stride is zero."""
     run(driver, "one")
+
+
+def test_rows_of_outputs_lie_apart(driver):
+    """Outputs whose rows overlap are refused, others are taken in any order."""
+    run(driver, "apart")
