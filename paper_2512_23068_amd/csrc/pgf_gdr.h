@@ -61,9 +61,11 @@ __device__ __forceinline__ int64_t uni(int64_t x) {
 
 // Rows of one head from some step on, read and written through a buffer
 // descriptor: what lies behind the last live row reads as zero and is not
-// written, without a branch or a comparison.  A lane whose element is not
-// there gives the offset kNone.  The byte offset of row t is t * st; st is
-// below 2^24 (checked on the host), a chunk below 2^30.
+// written, without a branch or a comparison, as long as rows lie at least their
+// width apart (an output's do).  Of an input whose step stride is less, the rows
+// behind the last live one read as what lies there of that row.  A lane whose
+// element is not there gives the offset kNone.  The byte offset of row t is
+// t * st; st is below 2^24 (checked on the host), a chunk below 2^30.
 constexpr uint32_t kNone = 0x80000000u;
 struct Buf {
     __amdgpu_buffer_rsrc_t r;

@@ -337,8 +337,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
             for (int j = 0; j < 4; ++j) store1<float>(ob, so, place(kt, j), S[kt][j]);
     };
 
-    // What this thread stages of a chunk.  Rows behind the sequence's end read
-    // as zero; their beta is zero in the record, so they write nothing.
+    // What this thread stages of a chunk.  Rows behind the sequence's end have a
+    // beta of zero in the record, so they write nothing, whatever is read there
+    // (zero, or where rows overlap, of the last one).
     Raw8<T> rk[KU], rq[OUT ? KU : 1];
     uintx4 rm[MU];
     float reG;

@@ -157,6 +157,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 
     if (chunks > 0) {
         fetch(chunks - 1);
+        // dO's rows behind the end are inside its buffer where its step stride is
+        // below a row.  (With them zero, Q's, K's and V's there count for nothing.)
+        const int live = live_rows(chunks - 1);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ro[m][j] = 16 * m + 4 * qd + j < live ? ro[m][j] : 0u;
 #pragma unroll
         for (int i = 0; i < NB; ++i) zero_tile<NI, 256>(lds[i].M, tid);
         stage(lds[0]);
@@ -377,7 +384,8 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
         re.y = *(const uintx4 *)(ep + 4);
         if constexpr (SIDE == 1) {
             const Buf gb = make_buf(row_ptr<T>(a.go, r.b, h, t0), (uint32_t)a.go.st * sizeof(T), live, a.dv * (int)sizeof(T));
-            rg = load8<T>(gb, con ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
+            // (a step stride below a row leaves rows behind the end inside the buffer)
+            rg = load8<T>(gb, con && er < live ? er * gb.st + vc * (uint32_t)sizeof(T) : kNone, 0);
         }
     };
     auto gates = [&](int vh) {

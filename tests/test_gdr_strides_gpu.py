@@ -57,3 +57,53 @@ def test_one_step_into_given_outputs(dtype, B, Hk, Hv, dk, dv, sliced):
     compare(got, reference(c, do, dk ** -0.5, S0, dS1), dtype)
     if sliced:
         assert all(bool((x[:, :, [0, 1, 2, 4]] == 7).all()) for x in whole)
+
+
+def spread(x, kind):
+    """x [B,H,L,d] with one row for all steps, or with rows that begin 16 bytes after
+    each other, on the CPU and on the GPU."""
+    B, H, L, d = x.shape
+    if kind == "broadcast":
+        return x[:, :, :1].expand(B, H, L, d), x[:, :, :1].to(DEV).expand(B, H, L, d)
+    unit = 16 // x.element_size()
+    n = d + unit * (L - 1)
+    flat = x.flatten(2)[..., :n].contiguous()
+    return tuple(f.as_strided(x.shape, (H * n, n, unit, 1)) for f in (flat, flat.to(DEV)))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["broadcast", "window"])
+@pytest.mark.parametrize("which", ["q do", "q k v do"])
+@pytest.mark.parametrize("B,Hk,Hv,L,dk,dv,cu", [
+    (2, 2, 4, 33, 64, 64, None), (1, 2, 2, 70, 128, 40, None), (2, 1, 2, 65, 24, 136, None),
+    (1, 2, 4, 100, 64, 64, [0, 33, 34, 100])])
+def test_broadcast_and_window_inputs(dtype, kind, which, B, Hk, Hv, L, dk, dv, cu):
+    """Step strides below a row: what follows a sequence's last row in memory is the
+    array's own, and does not count."""
+    print(f"case {dtype} {kind} {which} {B} {Hk} {Hv} {L} {dk} {dv}", flush=True)
+    c, d = (list(x) for x in make(B, Hk, Hv, L, dk, dv, dtype, seed=83))
+    gen = torch.Generator().manual_seed(84)
+    do = torch.randn(B, Hv, L, dv, generator=gen).to(dtype)
+    dod = do.to(DEV)
+    for i, n in enumerate("qkv"):
+        if n in which.split():
+            c[i], d[i] = spread(c[i], kind)
+    if kind == "window" and "k" in which.split():      # (keys stay near norm 1: a window of normalised keys)
+        c[1], d[1] = spread(make(B, Hk, Hv, L, dk, dv, dtype, seed=85)[0][1], kind)
+    do, dod = spread(do, kind)
+    n = B if cu is None else len(cu) - 1
+    S0, dS1 = (torch.randn(n, Hv, dk, dv, generator=gen) * 0.5 for _ in range(2))
+    kw = {} if cu is None else dict(cu_seqlens=torch.tensor(cu, device=DEV, dtype=torch.int32))
+    o, S = binding.gdr_scan(*d, S_in=S0.to(DEV), return_state=True, **kw)
+    got = binding.gdr_grads(*d, dod, S_in=S0.to(DEV), dS_out=dS1.to(DEV), **kw)
+    if cu is None:
+        ro, rS = ref.scan(*c, dk ** -0.5, S0)
+        want = reference(c, do, dk ** -0.5, S0, dS1)
+    else:
+        parts = ref.packed(lambda *a: ref.scan(*a[:5], dk ** -0.5, a[5]), cu, c, [S0])
+        ro, rS = torch.cat([p[0] for p in parts], 2), torch.cat([p[1] for p in parts])
+        parts = ref.packed(lambda *a: reference(a[:5], a[5], dk ** -0.5, a[6], a[7]), cu, (*c, do), [S0, dS1])
+        want = [torch.cat([p[i] for p in parts], 2) for i in range(5)] + [torch.cat([p[5] for p in parts])]
+    check("o", o, ro, TOL[dtype])
+    check("S", S, rS, TOL[F32])
+    compare(got, want, dtype)
