@@ -306,12 +306,15 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
         for (int i = 0; i < 2; ++i) {
             for (int j = 0; j < 4; ++j) {
                 if (!overlaps(outs[i], ins[j])) continue;
-                // An output over an input: only its own, element on element.
+                // An output over an input: only its own, element on element (an
+                // index of one value has no stride to differ in).
+                const int64_t n[3] = {pl.B, outs[i].H, pl.L};
                 int64_t x[3], y[3];
                 dense_strides(outs[i].s, outs[i].H, pl.L, pl.d, x);
                 dense_strides(ins[j].s, ins[j].H, pl.L, pl.d, y);
-                if (j % 2 != i || outs[i].p != ins[j].p || x[0] != y[0] || x[1] != y[1] || x[2] != y[2])
-                    return PGF_ERR_INVALID_ARG;
+                bool same = j % 2 == i && outs[i].p == ins[j].p;
+                for (int e = 0; e < 3; ++e) same = same && (n[e] == 1 || x[e] == y[e]);
+                if (!same) return PGF_ERR_INVALID_ARG;
             }
             if (overlaps(p->workspace, pl.total, outs[i].p, outs[i].bytes())) return PGF_ERR_INVALID_ARG;
         }
