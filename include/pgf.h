@@ -470,7 +470,9 @@ int pgf_gdr_step(const void *q, const void *k, const void *v, const float *g, co
  * their accuracy.
  *   q, q_out [B, q_heads, L, d]    k, k_out [B, k_heads, L, d]
  * with strides as in the gated delta rule.  Either of q and k may be left out
- * (its heads 0).  An output may be its input (same address and strides).
+ * (its heads 0).  An output may be its input (same address and strides); else
+ * what is written, the weights' gradients and the workspace among it, overlaps
+ * nothing that is read and nothing else that is written.
  * ------------------------------------------------------------------------ */
 #define PGF_NORM_NONE 0
 #define PGF_NORM_L2   1

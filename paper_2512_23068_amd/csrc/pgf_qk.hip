@@ -316,9 +316,26 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
                 for (int e = 0; e < 3; ++e) same = same && (n[e] == 1 || x[e] == y[e]);
                 if (!same) return PGF_ERR_INVALID_ARG;
             }
-            if (overlaps(p->workspace, pl.total, outs[i].p, outs[i].bytes())) return PGF_ERR_INVALID_ARG;
         }
         if (overlaps(outs[0], outs[1])) return PGF_ERR_INVALID_ARG;
+        // The dense arrays: what is written (first the outputs, then the weights'
+        // gradients and the workspace) lies apart from what is read and from each other.
+        struct Range { const void *p; size_t n; };
+        const size_t nw = (size_t)pl.d * 4, nf = (size_t)pl.rot / 2 * 4;
+        const size_t np = pl.rot ? (size_t)((pl.B - 1) * p->pos_stride + pl.L) * (size_t)(p->pos_bits / 8) : 0;
+        const Range written[] = {{outs[0].p, outs[0].bytes()}, {outs[1].p, outs[1].bytes()},
+                                 {grads && p->w_q ? p->grad_w_q : nullptr, nw}, {grads && p->w_k ? p->grad_w_k : nullptr, nw},
+                                 {grads ? p->workspace : nullptr, pl.total}};
+        const Range read[] = {{p->w_q, nw}, {p->w_k, nw}, {p->inv_freq, nf}, {p->positions, np}};
+        for (int i = 0; i < 5; ++i) {
+            for (const auto &x : read)
+                if (overlaps(written[i].p, written[i].n, x.p, x.n)) return PGF_ERR_INVALID_ARG;
+            if (i < 2) continue;
+            for (const auto &x : ins)
+                if (overlaps(written[i].p, written[i].n, x.p, x.bytes())) return PGF_ERR_INVALID_ARG;
+            for (int j = 0; j < i; ++j)
+                if (overlaps(written[i].p, written[i].n, written[j].p, written[j].n)) return PGF_ERR_INVALID_ARG;
+        }
     }
     (void)hipGetLastError();
     hipStream_t st = (hipStream_t)stream;

@@ -31,3 +31,37 @@ def test_rows_of_prepared_queries(strides):
     good = [A + i * GB for i in range(4)]
     p = qk(q_out_strides=strides)
     assert binding.lib().pgf_qk_norm(good[0], good[1], ctypes.byref(p), good[2], good[3], None) == INVALID
+
+
+def test_overlaps_of_preparation():
+    """Outputs (the weights' gradients and the workspace among them) over any input,
+    or over each other."""
+    lib = binding.lib()
+    at = {n: A + i * GB for i, n in enumerate(("q", "k", "dq", "dk", "q_out", "k_out", "w_q", "w_k", "inv_freq", "positions",
+                                              "grad_w_q", "grad_w_k", "workspace"))}
+    n = lib.pgf_qk_norm_workspace_bytes(ctypes.byref(qk(w_q=A, w_k=A)))
+
+    def call(fn="pgf_qk_norm_grads", **move):
+        x = {**at, **move}
+        p = qk(pos_bits=64, pos_stride=10, workspace_bytes=n, **{k: x[k] for k in (
+            "w_q", "w_k", "inv_freq", "positions", "grad_w_q", "grad_w_k", "workspace")})
+        if fn == "pgf_qk_norm":
+            return lib.pgf_qk_norm(x["q"], x["k"], ctypes.byref(p), x["q_out"], x["k_out"], None)
+        return lib.pgf_qk_norm_grads(x["q"], x["k"], x["dq"], x["dk"], ctypes.byref(p), x["q_out"], x["k_out"], None)
+
+    small = {"w_q": 256, "w_k": 256, "inv_freq": 128, "positions": 2 * 10 * 8, "grad_w_q": 256, "grad_w_k": 256}
+    ins = ("q", "k", "dq", "dk", "w_q", "w_k", "inv_freq", "positions")
+    for o in ("grad_w_q", "grad_w_k", "workspace", "q_out", "k_out"):
+        for i in ins:
+            # the output's first bytes on the input's last ones
+            last = at[i] + (small[i] - 4 if i in small else 256)
+            if o not in small:
+                last = last // 256 * 256 if last % 256 else last
+            if (o, i) in (("q_out", "q"), ("k_out", "k"), ("q_out", "dq"), ("k_out", "dk")):
+                last = at[i] + 256                 # (on its own input it may lie, not beside)
+            assert call(**{o: last}) == INVALID, (o, i)
+    for o, i in (("grad_w_q", "grad_w_k"), ("grad_w_q", "q_out"), ("grad_w_k", "k_out"), ("grad_w_q", "workspace"),
+                 ("workspace", "q_out"), ("workspace", "k_out")):
+        assert call(**{o: at[i]}) == INVALID, (o, i)
+    for i in ("w_q", "w_k", "inv_freq", "positions"):
+        assert call("pgf_qk_norm", q_out=at[i]) == INVALID, i
