@@ -436,8 +436,8 @@ size_t pgf_gdr_workspace_bytes(const pgf_gdr_params *p);
  * cut) in *seg_len.  Host only.  Returns a status. */
 int pgf_gdr_plan(const pgf_gdr_params *p, int32_t *seg_len);
 
-/* The scan over whole sequences.  o must not overlap an input, nor the
- * workspace anything. */
+/* The scan over whole sequences.  o and S_out must not overlap an input
+ * (cu_seqlens is one; S_out may be S_in), nor the workspace anything. */
 int pgf_gdr_scan(const void *q, const void *k, const void *v, const float *g, const float *beta,
                  const pgf_gdr_params *p, void *o, void *stream);
 

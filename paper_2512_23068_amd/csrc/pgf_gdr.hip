@@ -268,9 +268,11 @@ extern "C" int pgf_gdr_scan(const void *q, const void *k, const void *v, const f
     const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;
     const Arr out{o, p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e};
     const size_t ns = (size_t)(pl.nseq * pl.Hv * pl.dk * pl.dv) * 4;
+    const int64_t dense[3] = {0, 0, 0};
     const Arr ins[] = {{q, p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {k, p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
                        {v, p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {g, p->g_strides, pl.B, pl.Hv, pl.L, 1, 4},
-                       {beta, p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4}};
+                       {beta, p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4},
+                       {p->n_seqs ? p->cu_seqlens : nullptr, dense, 1, 1, 1, pl.nseq + 1, 4}};
     for (const auto &i : ins)
         if (overlaps(out, i) || overlaps(p->workspace, pl.total, i.p, i.bytes()) || overlaps(p->S_out, ns, i.p, i.bytes()))
             return PGF_ERR_INVALID_ARG;

@@ -823,7 +823,8 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     const Arr ins[] = {{q, p->q_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {k, p->k_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
                        {v, p->v_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {do_, p->o_strides, pl.B, pl.Hv, pl.L, pl.dv, e},
                        {g, p->g_strides, pl.B, pl.Hv, pl.L, 1, 4}, {beta, p->beta_strides, pl.B, pl.Hv, pl.L, 1, 4},
-                       {p->S_in, dense, 1, 1, 1, (int64_t)ns, 1}, {p->dS_out, dense, 1, 1, 1, (int64_t)ns, 1}};
+                       {p->S_in, dense, 1, 1, 1, (int64_t)ns, 1}, {p->dS_out, dense, 1, 1, 1, (int64_t)ns, 1},
+                       {p->n_seqs ? p->cu_seqlens : nullptr, dense, 1, 1, 1, pl.nseq + 1, 4}};
     const Arr outs[] = {{dq, p->dq_strides, pl.B, pl.Hk, pl.L, pl.dk, e}, {dk, p->dk_strides, pl.B, pl.Hk, pl.L, pl.dk, e},
                         {dv, p->dv_strides, pl.B, pl.Hv, pl.L, pl.dv, e}, {dg, dense, 1, 1, 1, (int64_t)ng, 1},
                         {dbeta, dense, 1, 1, 1, (int64_t)ng, 1}, {p->dS_in, dense, 1, 1, 1, (int64_t)ns, 1}};

@@ -65,3 +65,25 @@ def test_overlaps_of_preparation():
         assert call(**{o: at[i]}) == INVALID, (o, i)
     for i in ("w_q", "w_k", "inv_freq", "positions"):
         assert call("pgf_qk_norm", q_out=at[i]) == INVALID, i
+
+
+def _packed(fn, **kw):
+    """A packed call of made-up addresses that is refused for what kw says (or for its workspace)."""
+    p = gdr(batch=1, n_seqs=3, **kw)
+    x = [A + i * GB for i in range(11)]
+    lib = binding.lib()
+    if fn == "pgf_gdr_scan":
+        return lib.pgf_gdr_scan(*x[:5], ctypes.byref(p), x[5], None)
+    return lib.pgf_gdr_grads(*x[:6], ctypes.byref(p), *x[6:], None)
+
+
+@pytest.mark.parametrize("fn", ["pgf_gdr_scan", "pgf_gdr_grads"])
+def test_bounds_of_packed_sequences_are_inputs(fn):
+    """cu_seqlens under an output, a state that is written, or the workspace."""
+    n = binding.lib().pgf_gdr_workspace_bytes(ctypes.byref(gdr(batch=1, n_seqs=3, grads=1)))
+    ws = dict(workspace=A + 20 * GB, workspace_bytes=n)
+    for o in range(5, 6) if fn == "pgf_gdr_scan" else range(6, 11):
+        assert _packed(fn, cu_seqlens=A + o * GB, **ws) == INVALID, o
+    assert _packed(fn, cu_seqlens=A + 20 * GB + 64, **ws) == INVALID
+    state = "S_out" if fn == "pgf_gdr_scan" else "dS_in"
+    assert _packed(fn, cu_seqlens=A + 30 * GB + 4, **{state: A + 30 * GB}, **ws) == INVALID
