@@ -373,8 +373,9 @@ int pgf_la_scan_jvp(const float *q, const float *k, const float *v, const float 
  * Rows of outputs lie apart (ordered by stride, each index that moves steps over
  * all that the ones before it span).
  * q, k, v, o and their gradients are f32 or bf16 (in_dtype); the arrays'
- * addresses and strides are multiples of 16 bytes (g and beta: of 4), a step's
- * stride below 2^24 bytes.
+ * addresses (S_pool's too) and strides are multiples of 16 bytes (g, beta, their
+ * gradients, other states, bounds and slots: of 4), a step's stride below 2^24
+ * bytes.
  *
  * Packed sequences: with n_seqs > 0, batch is 1 and the rows of the one
  * batch entry hold n_seqs sequences; sequence n has the rows cu_seqlens[n]

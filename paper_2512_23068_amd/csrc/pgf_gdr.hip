@@ -185,6 +185,9 @@ Args make_args(const Plan &pl, const pgf_gdr_params *p, const void *q, const voi
 int check_arrays(const Plan &pl, const pgf_gdr_params *p, const void *q, const void *k, const void *v, const float *g,
                  const float *beta, const void *o) {
     if (p->n_seqs && !p->cu_seqlens) return PGF_ERR_INVALID_ARG;
+    if (((uintptr_t)p->cu_seqlens | (uintptr_t)p->slots | (uintptr_t)p->S_in | (uintptr_t)p->S_out | (uintptr_t)p->dS_out |
+         (uintptr_t)p->dS_in) & 3)
+        return PGF_ERR_INVALID_ARG;
     if (pl.L == 0) return PGF_OK;
     if (!q || !k || !v || !g || !beta || !o) return PGF_ERR_INVALID_ARG;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) return PGF_ERR_INVALID_ARG;

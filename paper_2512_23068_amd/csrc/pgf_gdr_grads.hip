@@ -816,6 +816,7 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     if (rc != PGF_OK) return rc;
     if (pl.L > 0 && (!dq || !dk || !dv || !dg || !dbeta)) return PGF_ERR_INVALID_ARG;
     if (((uintptr_t)dq | (uintptr_t)dk | (uintptr_t)dv) & 15) return PGF_ERR_INVALID_ARG;
+    if (((uintptr_t)dg | (uintptr_t)dbeta) & 3) return PGF_ERR_INVALID_ARG;
     if (!p->workspace || p->workspace_bytes < pl.total || ((uintptr_t)p->workspace & 255)) return PGF_ERR_WORKSPACE;
     const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;
     const size_t ns = (size_t)(pl.nseq * pl.Hv * pl.dk * pl.dv) * 4, ng = (size_t)(pl.B * pl.Hv * pl.L) * 4;

@@ -286,6 +286,10 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
     const int rc = make_plan(p, &pl, grads);
     if (rc != PGF_OK) return rc;
     if (grads && ((p->w_q && pl.Hq && !p->grad_w_q) || (p->w_k && pl.Hk && !p->grad_w_k))) return PGF_ERR_INVALID_ARG;
+    if (((uintptr_t)p->w_q | (uintptr_t)p->w_k | (uintptr_t)p->inv_freq |
+         (grads ? (uintptr_t)p->grad_w_q | (uintptr_t)p->grad_w_k : 0)) & 3)
+        return PGF_ERR_INVALID_ARG;
+    if (pl.rot && p->positions && (uintptr_t)p->positions % (size_t)(p->pos_bits / 8)) return PGF_ERR_INVALID_ARG;
     if (grads && pl.total && (!p->workspace || p->workspace_bytes < pl.total || ((uintptr_t)p->workspace & 255)))
         return PGF_ERR_WORKSPACE;
     const size_t e = p->in_dtype == PGF_BF16 ? 2 : 4;

@@ -87,3 +87,33 @@ def test_bounds_of_packed_sequences_are_inputs(fn):
     assert _packed(fn, cu_seqlens=A + 20 * GB + 64, **ws) == INVALID
     state = "S_out" if fn == "pgf_gdr_scan" else "dS_in"
     assert _packed(fn, cu_seqlens=A + 30 * GB + 4, **{state: A + 30 * GB}, **ws) == INVALID
+
+
+def test_addresses_of_small_arrays():
+    """States, bounds, slots and f32 gradients at addresses that are no multiple of
+    their element."""
+    n = binding.lib().pgf_gdr_workspace_bytes(ctypes.byref(gdr(batch=1, n_seqs=3, grads=1)))
+    ws = dict(workspace=A + 20 * GB, workspace_bytes=n, cu_seqlens=A + 40 * GB)
+    x = [A + i * GB for i in range(11)]
+    lib = binding.lib()
+    for kw in (dict(S_in=A + 30 * GB + 2), dict(S_out=A + 30 * GB + 1), dict(cu_seqlens=A + 30 * GB + 2)):
+        p = gdr(batch=1, n_seqs=3, **{**ws, **kw})
+        assert lib.pgf_gdr_scan(*x[:5], ctypes.byref(p), x[5], None) == INVALID, kw
+    for kw in (dict(S_in=A + 30 * GB + 2), dict(dS_out=A + 30 * GB + 1), dict(dS_in=A + 30 * GB + 2),
+               dict(cu_seqlens=A + 30 * GB + 2)):
+        p = gdr(batch=1, n_seqs=3, **{**ws, **kw})
+        assert lib.pgf_gdr_grads(*x[:6], ctypes.byref(p), *x[6:], None) == INVALID, kw
+    for o in (9, 10):
+        y = [a + 2 * (i == o) for i, a in enumerate(x)]
+        p = gdr(batch=1, n_seqs=3, **ws)
+        assert lib.pgf_gdr_grads(*y[:6], ctypes.byref(p), *y[6:], None) == INVALID, o
+    p = gdr(seqlen=1, S_pool=A + 20 * GB, pool=2, slots=A + 30 * GB + 2)
+    assert lib.pgf_gdr_step(*x[:5], ctypes.byref(p), x[5], None) == INVALID
+    m = lib.pgf_qk_norm_workspace_bytes(ctypes.byref(qk(w_q=A, w_k=A)))
+    good = dict(w_q=A + 10 * GB, w_k=A + 11 * GB, inv_freq=A + 12 * GB, positions=A + 13 * GB, grad_w_q=A + 14 * GB,
+                grad_w_k=A + 15 * GB)
+    for bits in (32, 64):
+        for name in good:
+            p = qk(**{**good, name: good[name] + (4 if name == "positions" and bits == 64 else 2)}, pos_bits=bits, pos_stride=10,
+                   workspace=A + 20 * GB, workspace_bytes=m)
+            assert lib.pgf_qk_norm_grads(*x[:4], ctypes.byref(p), x[4], x[5], None) == INVALID, (name, bits)
