@@ -44,11 +44,6 @@ __device__ __forceinline__ uint32_t xcd_item(uint32_t b, uint32_t run) {
     const uint32_t x = b % 8, i = b / 8;
     return (i / run * 8 + x) * run + i % run;
 }
-// Blocks for n items.
-inline unsigned xcd_grid(int64_t n, int64_t run) {
-    const int64_t runs = (n + run - 1) / run;
-    return (unsigned)((runs + 7) / 8 * 8 * run);
-}
 
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));

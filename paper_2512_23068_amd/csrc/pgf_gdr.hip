@@ -213,18 +213,17 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
             s.ct = a.vt + (int)((pl.dk + 15) / 16);
             const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment, 1>), dim3(xcd_grid(items, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, items);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment, 1>), dim3((unsigned)xcd_grid(items, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, items);
         }
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3(xcd_grid(pl.nseq * pl.Hv * a.vt, a.vt)), dim3(4 * DK), 0, st, a);
+        hipLaunchKernelGGL((k_gdr_carry<DK, false>), dim3((unsigned)xcd_grid(pl.nseq * pl.Hv * a.vt, a.vt)), dim3(4 * DK), 0, st, a);
         a.seg_in = a.segE;
     }
     Timed tm(3, st);
-    const int share = pl.seg_slots * pl.Hv * a.ct <= kShareTiles ? 2 : 1;
-    const int cb = (a.ct + 4 / share - 1) / (4 / share);
+    const int cb = (a.ct * pl.share + 3) / 4;
     const uint32_t items = (uint32_t)(pl.seg_slots * pl.Hv * cb);
-    const dim3 grid(xcd_grid(items, cb * a.rep));
-    if (share == 2) hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut, 2>), grid, dim3(256), 0, st, a, items);
+    const dim3 grid((unsigned)xcd_grid(items, cb * a.rep));
+    if (pl.share == 2) hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut, 2>), grid, dim3(256), 0, st, a, items);
     else hipLaunchKernelGGL((k_gdr_chain<T, DK, kOut, 1>), grid, dim3(256), 0, st, a, items);
     return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;
 }
@@ -232,24 +231,14 @@ int scan_t(Args a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
 template <typename T>
 int step_t(const Args &a, const Plan &pl, const pgf_gdr_params *p, hipStream_t st) {
     Timed tm(3, st);
-    const int64_t bh = pl.B * pl.Hv;
-#define PGF_STEP(DK_, CB_)                                                                                         \
-    {                                                                                                              \
-        const uint32_t items = (uint32_t)(bh * ((pl.dv + CB_ - 1) / CB_));                                         \
-        hipLaunchKernelGGL((k_gdr_step<T, DK_, CB_>), dim3(xcd_grid(items, (pl.dv + CB_ - 1) / CB_)), dim3(256), 0, st, a, p->S_pool, p->pool,        \
-                           p->slots, pl.L, items);                                                                 \
-    }
-    // 32 value columns a block for one or two steps: more blocks have loads in
-    // flight (one step of 4096 states of 128 x 128 95 us, with 128 columns a block
-    // 94; of 1024 states 24.8 and 26.7).  Further steps wait for each other within
-    // a block, and a quarter of the blocks wait a quarter of the time once there is
-    // more than the GPU holds (16 steps of 2048 states 247 us, with 128 columns a
-    // block 139; of 256 states 44 and 38, 4 steps of 256 states 16 and 16).
-    const bool wide = pl.L > 2 && bh * ((pl.dv + 127) / 128) >= 256;
+    const int64_t cb = (pl.dv + pl.step_cols - 1) / pl.step_cols, items = pl.B * pl.Hv * cb;
+    const dim3 grid((unsigned)xcd_grid(items, cb));
+#define PGF_STEP(DK_, CB_) \
+    hipLaunchKernelGGL((k_gdr_step<T, DK_, CB_>), grid, dim3(256), 0, st, a, p->S_pool, p->pool, p->slots, pl.L, (uint32_t)items)
     if (pl.DK == 64) {
-        if (wide) PGF_STEP(64, 128) else PGF_STEP(64, 32)
+        if (pl.step_cols == 128) PGF_STEP(64, 128); else PGF_STEP(64, 32);
     } else {
-        if (wide) PGF_STEP(128, 128) else PGF_STEP(128, 32)
+        if (pl.step_cols == 128) PGF_STEP(128, 128); else PGF_STEP(128, 32);
     }
 #undef PGF_STEP
     return hipGetLastError() == hipSuccess ? PGF_OK : PGF_ERR_HIP;

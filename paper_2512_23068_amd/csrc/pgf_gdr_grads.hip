@@ -772,26 +772,26 @@ int grads_t(Args a, const Plan &pl, hipStream_t st) {
             s.ct = a.vt + (int)((pl.dk + 15) / 16);
             const uint32_t n = (uint32_t)(pl.seg_slots * pl.Hv * ((s.ct + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment, 1>), dim3(xcd_grid(n, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, n);
+            hipLaunchKernelGGL((k_gdr_chain<T, DK, kSegment, 1>), dim3((unsigned)xcd_grid(n, (s.ct + 3) / 4 * a.rep)), dim3(256), 0, st, s, n);
         }
         {
             const uint32_t n = (uint32_t)(pl.seg_slots * pl.Hv * ((a.vt + 3) / 4));
             Timed tm(1, st);
-            hipLaunchKernelGGL((k_gdr_back<T, DK, kBackSegment>), dim3(xcd_grid(n, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, n);
+            hipLaunchKernelGGL((k_gdr_back<T, DK, kBackSegment>), dim3((unsigned)xcd_grid(n, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, n);
         }
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_carry<DK, true>), dim3(xcd_grid(pl.nseq * pl.Hv * a.vt, a.vt), 2), dim3(4 * DK), 0, st, a);
+        hipLaunchKernelGGL((k_gdr_carry<DK, true>), dim3((unsigned)xcd_grid(pl.nseq * pl.Hv * a.vt, a.vt), 2), dim3(4 * DK), 0, st, a);
         a.seg_in = a.segE;
         a.dseg_in = a.dsegE;
     }
     const uint32_t blocks = (uint32_t)(pl.seg_slots * pl.Hv * ((a.ct + 3) / 4));
     if (items) {
         Timed tm(1, st);
-        hipLaunchKernelGGL((k_gdr_chain<T, DK, kSave, 1>), dim3(xcd_grid(blocks, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, blocks);
+        hipLaunchKernelGGL((k_gdr_chain<T, DK, kSave, 1>), dim3((unsigned)xcd_grid(blocks, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, blocks);
     }
     {
         Timed tm(2, st);
-        hipLaunchKernelGGL((k_gdr_back<T, DK, kBack>), dim3(xcd_grid(blocks, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, blocks);
+        hipLaunchKernelGGL((k_gdr_back<T, DK, kBack>), dim3((unsigned)xcd_grid(blocks, (a.vt + 3) / 4 * a.rep)), dim3(256), 0, st, a, blocks);
     }
     if (items) {
         Timed tm(3, st);

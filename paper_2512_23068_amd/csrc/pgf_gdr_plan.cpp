@@ -9,13 +9,17 @@ namespace pgf {
 
 namespace {
 
-constexpr int64_t kMaxBlocks = int64_t(1) << 30;
+constexpr int64_t kMaxItems = int64_t(1) << 30;
 constexpr int64_t kMaxHeads = int64_t(1) << 16, kMaxBatch = int64_t(1) << 24, kMaxLen = int64_t(1) << 32;
 constexpr int64_t kMaxStride = int64_t(1) << 44;
 constexpr int64_t kMaxStep = (int64_t(1) << 24) - 16;      // bytes from step to step
 constexpr size_t kMaxTotal = size_t(1) << 46;
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Whether a launch has fewer than 2^32 threads: of more, only the low 32 bits of
+// their number run, without an error (2^24 + 1 blocks of 256: one block).
+bool fits(int64_t blocks, int64_t threads) { return (double)blocks * (double)threads < 4294967296.0; }
 
 // Strides of an array of rows of `width` elements: not negative, bounded, in
 // units of 16 bytes.  An output's rows lie apart: of the indexes that move, in the
@@ -166,26 +170,46 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
     q.DK = q.dk <= 64 ? 64 : 128;
     q.nseq = p->n_seqs ? p->n_seqs : q.B;
-    // An upper bound of the blocks of one head; grids are padded by less than 8 key heads.
+    // An upper bound of the blocks of one head.
     const int64_t col_blocks = cdiv(q.dv, 16) + q.DK / 16;
     if (step) {
         if (p->pool < 0 || p->pool > kMaxLen) return PGF_ERR_INVALID_ARG;
-        if (q.B * q.Hv > kMaxBlocks / col_blocks) return PGF_ERR_UNSUPPORTED;
+        if (q.B * q.Hv > kMaxItems / col_blocks) return PGF_ERR_UNSUPPORTED;
+        // 32 value columns a block for one or two steps: more blocks have loads in
+        // flight (one step of 4096 states of 128 x 128 95 us, with 128 columns a block
+        // 94; of 1024 states 24.8 and 26.7).  Further steps wait for each other within
+        // a block, and a quarter of the blocks wait a quarter of the time once there is
+        // more than the GPU holds (16 steps of 2048 states 247 us, with 128 columns a
+        // block 139; of 256 states 44 and 38, 4 steps of 256 states 16 and 16).
+        q.step_cols = q.L > 2 && q.B * q.Hv * cdiv(q.dv, 128) >= 256 ? 128 : 32;
+        const int64_t cb = cdiv(q.dv, q.step_cols);
+        if (!fits(xcd_grid(q.B * q.Hv * cb, cb), 256)) return PGF_ERR_UNSUPPORTED;
         *out = q;
         return PGF_OK;
     }
     q.chunks_per = cdiv(q.L, kC);
     q.chunk_slots = p->n_seqs ? q.L / kC + p->n_seqs : q.B * q.chunks_per;
-    if (q.chunk_slots * q.Hv > kMaxBlocks / col_blocks || q.nseq * q.Hv > kMaxBlocks / col_blocks)
+    if (q.chunk_slots * q.Hv > kMaxItems / col_blocks || q.nseq * q.Hv > kMaxItems / col_blocks)
         return PGF_ERR_UNSUPPORTED;
     q.seg = p->seg_len > 0 ? p->seg_len : p->seg_len < 0 ? 0 : default_seg(q, p->n_seqs > 0, grads);
     if (q.seg >= q.L) q.seg = 0;
     q.segs_per = q.seg ? cdiv(q.L, q.seg) : 1;
     q.seg_slots = !q.seg ? q.nseq : p->n_seqs ? q.L / q.seg + p->n_seqs : q.B * q.segs_per;
-    const int64_t cell = q.Hv * q.dk * q.dv * 4, cell_tr = q.Hv * (int64_t)q.DK * q.DK * 4;
-    q.rec_bytes = kMatBytes * (grads ? 3 : 2) + 256;
     q.supers_per = cdiv(q.L, kSuper * kC);
     q.super_slots = p->n_seqs ? q.L / (kSuper * kC) + p->n_seqs : q.B * q.supers_per;
+    const int64_t vt = cdiv(q.dv, 16), kt = cdiv(q.dk, 16), rep = q.Hv / q.Hk;
+    q.share = !grads && q.seg_slots * q.Hv * vt <= kShareTiles ? 2 : 1;
+    // A block's four waves take `tiles` column tiles of a head, `waves` a tile.
+    auto heads = [&](int64_t tiles, int64_t waves) {
+        const int64_t cb = cdiv(tiles * waves, 4);
+        return fits(xcd_grid(q.seg_slots * q.Hv * cb, cb * rep), 256);
+    };
+    if (!fits(cdiv(q.chunk_slots * q.Hk, 4), 256) || !heads(vt, q.share) ||
+        (q.seg && (!heads(vt + kt, 1) || !fits(xcd_grid(q.nseq * q.Hv * vt, vt), 4 * q.DK))) ||
+        (grads && !fits(q.super_slots * q.Hk, 512)) || (p->n_seqs && p->clear_rest && !fits(cdiv(q.L, 64), 256)))
+        return PGF_ERR_UNSUPPORTED;
+    const int64_t cell = q.Hv * q.dk * q.dv * 4, cell_tr = q.Hv * (int64_t)q.DK * q.DK * 4;
+    q.rec_bytes = kMatBytes * (grads ? 3 : 2) + 256;
     const int64_t ns = q.seg ? q.seg_slots : 0, nc = grads ? q.chunk_slots : 0, nu = grads ? q.super_slots : 0;
     bool ok = section(&q.total, &q.rec, q.chunk_slots, q.Hv * q.rec_bytes);
     ok = ok && section(&q.total, &q.segE, ns, cell) && section(&q.total, &q.tr, ns, cell_tr);
@@ -224,13 +248,22 @@ int make_plan(const pgf_qk_params *p, Plan *out, bool grads) {
     for (const auto &a : arrays)
         if (!strides_ok(a.s, unit, a.out, q.B, a.heads, q.L, q.d)) return PGF_ERR_INVALID_ARG;
     if ((double)q.B * (double)(q.Hq + q.Hk) * (double)q.L * (double)q.d > 4e18) return PGF_ERR_UNSUPPORTED;
-    if ((double)q.B * (double)q.L > (double)kMaxBlocks) return PGF_ERR_UNSUPPORTED;
+    if ((double)q.B * (double)q.L > (double)kMaxItems) return PGF_ERR_UNSUPPORTED;
     q.G = 1;
     while (q.G * 8 < q.d) q.G *= 2;
+    // Steps per block: one while that leaves CUs without a few blocks, then as
+    // many as keep those (a block's start, with its angles, costs as much as a
+    // few vectors a lane: 16384 steps of 32 heads, two steps a block 112 us,
+    // eight 72).
+    const int64_t rows = q.B * q.L;
+    q.tb = 1;
+    while (q.tb < kTurn && rows / (2 * q.tb) >= 1024) q.tb *= 2;
+    // Blocks take further steps in turns where a launch would have too many.
+    q.blocks = std::min<int64_t>(cdiv(rows, q.tb), int64_t(1) << 23);
     // Blocks of the gradient kernel: enough to fill the GPU several times; each
     // leaves one partial sum of the weights' gradients.
-    q.blocks = std::min<int64_t>(std::max<int64_t>(1, q.B * q.L), 1024);
-    q.total = grads && (p->w_q || p->w_k) ? (size_t)q.blocks * 2 * q.d * sizeof(float) : 0;
+    q.grad_blocks = std::min<int64_t>(std::max<int64_t>(1, cdiv(rows, q.tb)), 1024);
+    q.total = grads && (p->w_q || p->w_k) ? (size_t)q.grad_blocks * 2 * q.d * sizeof(float) : 0;
     *out = q;
     return PGF_OK;
 }

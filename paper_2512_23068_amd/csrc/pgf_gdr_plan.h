@@ -17,6 +17,13 @@ constexpr int kSuper = 2;        // chunks between saved states of the gradients
 constexpr int64_t kShareTiles = 512;
 constexpr int64_t kMatBytes = 3 * 1024;  // a chunk's lower triangular matrix: three 16 x 16 tiles of f32
 
+// Blocks for n items in runs of `run` that are dealt to the 8 XCDs (xcd_item).  The
+// planner sees to it that a launch has fewer than 2^32 threads.
+inline int64_t xcd_grid(int64_t n, int64_t run) {
+    const int64_t runs = (n + run - 1) / run;
+    return (runs + 7) / 8 * 8 * run;
+}
+
 // Workspace sections (bytes, 256-byte aligned).
 //   rec   [chunk slots][Hv]                   k_gdr_prep's record of each chunk
 //   seg   [segment slots][Hv][dk][dv]         zero-start end state of a segment,
@@ -36,6 +43,8 @@ struct Plan {
     int64_t seg;                 // steps per segment, 0 = sequences are not cut
     int64_t seg_slots, segs_per;
     int64_t super_slots, supers_per;     // slots of kSuper * kC steps
+    int share;                   // waves that share a column tile of the scan's outputs
+    int step_cols;               // value columns of a block of single steps
     int64_t rec_bytes;           // of one chunk's record
     size_t rec, segE, tr, S, dS, u, du, trT, dseg, acc, total;
 };
@@ -47,10 +56,13 @@ int make_plan(const pgf_gdr_params *p, Plan *q, bool grads, bool step);
 
 namespace qk {
 
+constexpr int kTurn = 8;         // steps per block and turn at most
+
 struct Plan {
     int64_t B, Hq, Hk, L, d, rot;
     int G;                       // lanes per head
-    int64_t blocks;              // blocks of the gradient kernel
+    int tb;                      // steps per block and turn
+    int64_t blocks, grad_blocks; // blocks of the kernel, and of the gradients'
     size_t total;
 };
 int make_plan(const pgf_qk_params *p, Plan *q, bool grads);

@@ -56,7 +56,6 @@ __device__ __forceinline__ float group_sum(float v) {
 }
 
 constexpr int kPairs = 256;          // rotated pairs of a step at most
-constexpr int kTurn = 8;             // steps per block and turn at most
 
 // Rotation of a lane's runs (sgn = -1: back); cs: of its four pairs.
 __device__ __forceinline__ void rotate(floatx4 &x, floatx4 &y, const float2 *cs, int il, float sgn) {
@@ -365,22 +364,16 @@ int run(const void *q, const void *k, const void *dq, const void *dk, const pgf_
     a.H = (int)(pl.Hq + pl.Hk);
     a.eps = p->eps;
     a.c = p->norm == PGF_NORM_NONE ? 0.0f : p->norm == PGF_NORM_L2 ? 1.0f : 1.0f / (float)pl.d;
-    // Steps per block: one while that leaves CUs without a few blocks, then as
-    // many as keep those (a block's start, with its angles, costs as much as a
-    // few vectors a lane: 16384 steps of 32 heads, two steps a block 112 us,
-    // eight 66).
-    a.tb = 1;
-    while (a.tb < kTurn && a.rows / (2 * a.tb) >= 1024) a.tb *= 2;
-    const int64_t want = (a.rows + a.tb - 1) / a.tb;
+    a.tb = pl.tb;
     const bool bf = p->in_dtype == PGF_BF16;
     if (!grads) {
         if (a.rows == 0) return PGF_OK;
         Timed tm(0, st);
-        if (bf) launch<__bf16, false>(a, pl.G, (unsigned)want, st);
-        else launch<float, false>(a, pl.G, (unsigned)want, st);
+        if (bf) launch<__bf16, false>(a, pl.G, (unsigned)pl.blocks, st);
+        else launch<float, false>(a, pl.G, (unsigned)pl.blocks, st);
     } else {
         a.part = pl.total ? (float *)p->workspace : nullptr;
-        const unsigned blocks = (unsigned)(want < pl.blocks ? (want > 0 ? want : 1) : pl.blocks);
+        const unsigned blocks = (unsigned)pl.grad_blocks;
         {
             Timed tm(3, st);
             if (bf) launch<__bf16, true>(a, pl.G, blocks, st);
