@@ -166,7 +166,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     for (const auto &a : arrays)
         if (!strides_ok(a.s, a.unit, a.out, q.B, a.heads, q.L, a.width)) return PGF_ERR_INVALID_ARG;
     for (const auto &a : arrays)
-        if (q.L > 1 && a.s[2] * 16 / unit > kMaxStep) return PGF_ERR_UNSUPPORTED;
+        if (q.L > 1 && a.s[2] * (a.unit == 1 ? 4 : 16 / unit) > kMaxStep) return PGF_ERR_UNSUPPORTED;
     if ((double)q.B * (double)q.Hv * (double)q.L * (double)std::max(q.dk, q.dv) > 4e18) return PGF_ERR_UNSUPPORTED;
     q.DK = q.dk <= 64 ? 64 : 128;
     q.nseq = p->n_seqs ? p->n_seqs : q.B;

@@ -5,7 +5,7 @@ import ctypes
 import pytest
 
 from paper_2512_23068_amd import binding
-from tests.test_gdr_abi import A, GB, INVALID, OK, gdr, plan, qk
+from tests.test_gdr_abi import A, GB, INVALID, OK, UNSUPPORTED, gdr, plan, qk
 
 
 @pytest.mark.parametrize("kw,code", [
@@ -117,3 +117,10 @@ def test_addresses_of_small_arrays():
             p = qk(**{**good, name: good[name] + (4 if name == "positions" and bits == 64 else 2)}, pos_bits=bits, pos_stride=10,
                    workspace=A + 20 * GB, workspace_bytes=m)
             assert lib.pgf_qk_norm_grads(*x[:4], ctypes.byref(p), x[4], x[5], None) == INVALID, (name, bits)
+
+
+@pytest.mark.parametrize("name", ["g_strides", "beta_strides"])
+def test_steps_of_gates(name):
+    """A step's stride is below 2^24 bytes: 2^22 elements of f32."""
+    for step, code in (((1 << 22) - 4, OK), (1 << 21, OK), (1 << 22, UNSUPPORTED)):
+        assert plan(gdr(**{name: (0, 0, step)}))[0] == code, step
