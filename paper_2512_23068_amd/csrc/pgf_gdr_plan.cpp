@@ -78,20 +78,23 @@ bool overlaps(const Arr &a, const Arr &b) {
     int64_t x[3], y[3];
     dense_strides(a.s, a.H, a.L, a.width, x);
     dense_strides(b.s, b.H, b.L, b.width, y);
-    if (a.elem != b.elem || a.B != b.B || a.L != b.L) return true;
-    const int64_t e = (int64_t)a.elem, d = (int64_t)((intptr_t)b.p - (intptr_t)a.p);
-    // [0, m) and [d, d + n) repeated every `period` bytes
-    auto apart = [&](int64_t period, int64_t m, int64_t n) {
-        if (period <= 0) return false;
-        const int64_t off = (d % period + period) % period;
-        return off >= m && off + n <= period;
+    // Bytes modulo a stride: an index that steps by a multiple of it adds nothing, any
+    // other its whole span.  What lies in different places there lies apart.
+    const int64_t d = (int64_t)((intptr_t)b.p - (intptr_t)a.p);
+    auto span = [](const Arr &r, const int64_t (&s)[3], int64_t period) {
+        const int64_t n[3] = {r.B, r.H, r.L}, e = (int64_t)r.elem;
+        int64_t bytes = r.width * e;
+        for (int i = 0; i < 3; ++i)
+            if (s[i] * e % period) bytes += (n[i] - 1) * s[i] * e;
+        return bytes;
     };
-    const int64_t hx = (a.H - 1) * x[1] + a.width, hy = (b.H - 1) * y[1] + b.width;      // all heads of a step
-    const bool batches = a.B == 1 || x[0] == y[0];
-    if (a.B > 1 && batches && apart(x[0] * e, (hx + (a.L - 1) * x[2]) * e, (hy + (b.L - 1) * y[2]) * e)) return false;
-    if (a.L > 1 && x[2] == y[2] && batches && (a.B == 1 || (x[2] > 0 && x[0] % x[2] == 0)) &&
-        apart(x[2] * e, hx * e, hy * e))
-        return false;
+    const int64_t n[3] = {a.B, a.H, a.L};
+    for (int i = 0; i < 3; ++i) {
+        const int64_t period = x[i] * (int64_t)a.elem;
+        if (n[i] < 2 || period <= 0) continue;
+        const int64_t off = (d % period + period) % period;
+        if (off >= span(a, x, period) && off + span(b, y, period) <= period) return false;
+    }
     return true;
 }
 

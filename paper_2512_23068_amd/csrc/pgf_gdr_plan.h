@@ -85,8 +85,8 @@ struct Arr {
     size_t elem;
     size_t bytes() const { return extent(s, B, H, L, width, elem); }
 };
-// Whether two such arrays share memory.  Arrays whose rows interleave (parts of
-// one fused array: the same batch or step strides, apart within them) do not.
+// Whether two such arrays may share memory.  Arrays whose rows interleave (parts of
+// one fused array's rows, or of its heads' rows) do not.
 bool overlaps(const Arr &a, const Arr &b);
 
 }  // namespace pgf

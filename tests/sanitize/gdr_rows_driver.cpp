@@ -6,6 +6,8 @@
 //   one     arrays of one step, whatever stride their step index has
 //   apart   arrays of any length; and no two rows of an accepted output share an
 //           element
+//   parts   parts of one array's rows do not count as overlapping, in any order of
+//           batch, head and step, and arrays that share an element do
 #include <stdio.h>
 #include <string.h>
 
@@ -14,7 +16,60 @@
 
 #include "../../paper_2512_23068_amd/csrc/pgf_gdr_plan.h"
 
+// q, k and v (or their gradients) as parts of one array's rows.
+static int parts() {
+    std::mt19937_64 rng(9);
+    auto pick = [&](std::initializer_list<int64_t> v) { return *(v.begin() + rng() % v.size()); };
+    static char mem[1 << 20];
+    long apart = 0, shared = 0, failures = 0;
+    for (int i = 0; i < 20000; ++i) {
+        const int64_t n[3] = {pick({1, 2, 3}), pick({1, 2, 4}), pick({1, 2, 5})};
+        const int64_t w[2] = {pick({8, 16, 24}), pick({8, 16})}, gap = pick({0, 0, 8});
+        const bool inner = rng() % 2;              // each part's heads side by side, or heads of all parts
+        int order[3] = {0, 1, 2};
+        for (int k = 2; k > 0; --k) std::swap(order[k], order[rng() % (k + 1)]);
+        int64_t s[2][3], at, H[2] = {n[1], inner ? pick({1, 2, 4}) : n[1]};
+        if (inner) {                               // [.., step (or batch), heads of the first, heads of the second]
+            at = H[0] * w[0] + gap;
+            int64_t step = at + H[1] * w[1] + pick({0, 8});
+            for (int k = 0; k < 2; ++k) s[k][1] = w[k];
+            for (int k : order)
+                if (k != 1) {
+                    s[0][k] = s[1][k] = step;
+                    step *= n[k];
+                }
+        } else {                                   // rows [first, second] of any order
+            at = w[0] + gap;
+            int64_t step = at + w[1] + pick({0, 8});
+            for (int k : order) {
+                s[0][k] = s[1][k] = step;
+                step *= n[k];
+            }
+        }
+        const int64_t move = rng() % 2 ? 0 : pick({-8, 8, 16});      // (the second part out of its place)
+        if (at + move < 0) continue;
+        const pgf::Arr a{mem, s[0], n[0], H[0], n[2], w[0], 2}, b{mem + 2 * (at + move), s[1], n[0], H[1], n[2], w[1], 2};
+        std::set<int64_t> first;
+        bool hit = false;
+        for (int k = 0; k < 2; ++k)
+            for (int64_t x = 0; x < n[0]; ++x)
+                for (int64_t h = 0; h < H[k]; ++h)
+                    for (int64_t t = 0; t < n[2]; ++t)
+                        for (int64_t e = 0; e < w[k]; ++e) {
+                            const int64_t y = x * s[k][0] + h * s[k][1] + t * s[k][2] + e + (k ? at + move : 0);
+                            if (!k) first.insert(y);
+                            else hit |= first.count(y) > 0;
+                        }
+        (hit ? shared : apart) += 1;
+        const bool found = pgf::overlaps(a, b) || pgf::overlaps(b, a);
+        if (hit ? !(pgf::overlaps(a, b) && pgf::overlaps(b, a)) : !move && found) ++failures;
+    }
+    printf("%ld pairs apart, %ld share elements, %ld failures\n", apart, shared, failures);
+    return apart > 1000 && shared > 1000 ? 0 : 1;
+}
+
 int main(int argc, char **argv) {
+    if (argc > 1 && !strcmp(argv[1], "parts")) return parts();
     const bool one = argc > 1 && !strcmp(argv[1], "one");
     std::mt19937_64 rng(7);
     auto pick = [&](std::initializer_list<int64_t> v) { return *(v.begin() + rng() % v.size()); };

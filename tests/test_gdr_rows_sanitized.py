@@ -34,3 +34,8 @@ def test_rows_of_one_step(driver):
 def test_rows_of_outputs_lie_apart(driver):
     """Outputs whose rows overlap are refused, others are taken in any order."""
     run(driver, "apart")
+
+
+def test_parts_of_one_array(driver):
+    """Parts of one array's rows are taken, head by head too."""
+    run(driver, "parts")

@@ -107,3 +107,15 @@ def test_broadcast_and_window_inputs(dtype, kind, which, B, Hk, Hv, L, dk, dv, c
     check("o", o, ro, TOL[dtype])
     check("S", S, rS, TOL[F32])
     compare(got, want, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_grads_into_rows_of_heads(dtype):
+    """dq, dk and dv as parts of each head's rows [B, H, L, 3 d]."""
+    c, d = make(2, 3, 3, 70, 64, 64, dtype, seed=86)
+    do = torch.randn(2, 3, 70, 64, device=DEV).to(dtype)
+    want = binding.gdr_grads(*d, do)
+    big = torch.empty(2, 3, 70, 192, device=DEV, dtype=dtype)
+    got = binding.gdr_grads(*d, do, out=big.split(64, -1))
+    assert all(torch.equal(x, y) for x, y in zip(got, want))
+    assert torch.equal(big, torch.cat(want[:3], -1))
