@@ -745,7 +745,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int64_t t0 = uni(r.lo + r.unit0);
     const int64_t slot0 = uni(a.seqs.slot0(r.n, kC, a.chunk_per) + r.unit0 / kC);
 
-    float *const accq = a.acc + (sslot * a.Hk + hk) * (int64_t)(2 * kRun * a.dk), *const acck = accq + kRun * a.dk;
+    // (with one value head a key head nothing is kept there, and its first bytes are read in vain)
+    float *const accq = a.acc + (a.rep > 1 ? (sslot * a.Hk + hk) * (int64_t)(2 * kRun * a.dk) : 0);
+    float *const acck = accq + (a.rep > 1 ? kRun * a.dk : 0);
     // (the sides pass the same number of barriers)
     if (wv < 4) outer_side<T, DK, 0>(a, lds, r, t0, live, slot0, sslot, hk, w, accq, acck);
     else outer_side<T, DK, 1>(a, lds, r, t0, live, slot0, sslot, hk, w, accq, acck);
@@ -859,7 +861,7 @@ extern "C" int pgf_gdr_grads(const void *q, const void *k, const void *v, const 
     a.saveE = (float *)(ws + pl.u);
     a.saveU = (float *)(ws + pl.du);
     a.dsegE = (float *)(ws + pl.dseg);
-    a.acc = (float *)(ws + pl.acc);
+    a.acc = (float *)(ws + (a.rep > 1 ? pl.acc : pl.rec));
     a.save = kSuper;
     a.save_per = pl.supers_per;
     a.dg = dg;

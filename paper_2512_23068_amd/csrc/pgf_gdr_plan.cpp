@@ -219,7 +219,7 @@ int make_plan(const pgf_gdr_params *p, Plan *out, bool grads, bool step) {
     ok = ok && section(&q.total, &q.S, nu, cell) && section(&q.total, &q.dS, nu, cell);
     ok = ok && section(&q.total, &q.u, nc, q.Hv * kC * q.dv * 4) && section(&q.total, &q.du, nc, q.Hv * kC * q.dv * 4);
     ok = ok && section(&q.total, &q.trT, grads ? ns : 0, cell_tr) && section(&q.total, &q.dseg, grads ? ns : 0, cell);
-    ok = ok && section(&q.total, &q.acc, nu, q.Hk * 2 * kSuper * kC * q.dk * 4);
+    ok = ok && section(&q.total, &q.acc, rep > 1 ? nu : 0, q.Hk * 2 * kSuper * kC * q.dk * 4);
     if (!ok) return PGF_ERR_UNSUPPORTED;
     q.total = std::max<size_t>(q.total, 256);
     *out = q;

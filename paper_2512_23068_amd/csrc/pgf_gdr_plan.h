@@ -35,7 +35,8 @@ inline int64_t xcd_grid(int64_t n, int64_t run) {
 //   u, du [chunk slots][Hv][32][dv]           E and its adjoint of each chunk
 //   trT   [segment slots][Hv][DK][DK]         tr transposed
 //   dseg  [segment slots][Hv][dk][dv]         as seg, of the adjoint
-//   acc   [super slots][Hk][2][64][dk]        sums of dq and dk over value heads
+//   acc   [super slots][Hk][2][64][dk]        sums of dq and dk over value heads, where
+//                                             a key head has several
 struct Plan {
     int64_t B, Hk, Hv, L, dk, dv, nseq;
     int DK;                      // d_key padded to the kernels' 64 or 128

@@ -124,3 +124,15 @@ def test_steps_of_gates(name):
     """A step's stride is below 2^24 bytes: 2^22 elements of f32."""
     for step, code in (((1 << 22) - 4, OK), (1 << 21, OK), (1 << 22, UNSUPPORTED)):
         assert plan(gdr(**{name: (0, 0, step)}))[0] == code, step
+
+
+@pytest.mark.parametrize("Hk,Hv", [(4, 4), (2, 4), (1, 1)])
+def test_workspace_of_gradients(Hk, Hv):
+    """Records, states and errors with their adjoints; sums over value heads only
+    where a key head has several."""
+    B, L, dk, dv = 3, 150, 72, 40
+    p = gdr(batch=B, key_heads=Hk, value_heads=Hv, seqlen=L, d_key=dk, d_value=dv, grads=1, seg_len=-1)
+    chunks, runs = B * -(-L // 32), B * -(-L // 64)
+    parts = [chunks * Hv * (9 * 1024 + 256)] + 2 * [runs * Hv * dk * dv * 4] + 2 * [chunks * Hv * 32 * dv * 4]
+    parts += [runs * Hk * 2 * 64 * dk * 4] if Hv > Hk else []
+    assert binding.lib().pgf_gdr_workspace_bytes(ctypes.byref(p)) == sum(-(-x // 256) * 256 for x in parts)
