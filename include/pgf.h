@@ -467,8 +467,8 @@ int pgf_gdr_step(const void *q, const void *k, const void *v, const float *g, co
  * a weight per element (f32, NULL = 1).  R turns the pair (a, b) number i of
  * the first `rot` elements by the angle position * inv_freq[i]: the pairs are
  * the elements i and i + rot / 2, or 2 i and 2 i + 1 with `interleaved`.
- * Sums and angles are f32 (the angle's reduction f64), so far positions keep
- * their accuracy.
+ * Sums are f32; the angle, its sine and its cosine are f64, rounded once to f32,
+ * so far positions keep their accuracy.
  *   q, q_out [B, q_heads, L, d]    k, k_out [B, k_heads, L, d]
  * with strides as in the gated delta rule.  Either of q and k may be left out
  * (its heads 0).  An output may be its input (same address and strides); else
