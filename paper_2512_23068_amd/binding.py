@@ -622,12 +622,15 @@ def _bad(t, shape, dev, dtype, name):
     raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-def _rows(t, shape, dev, dtype, name):
+_FAR = 1 << 24
+
+
+def _rows(t, shape, dev, dtype, name, far=_FAR):
     """An input [B, H, L(, d)] as the kernels read it, and its strides {batch,
     head, step} (zero where the index does not move).  A tensor whose last index
-    is not dense, whose address or strides are not multiples of 16 bytes, or
-    that is one row for all indexes (strides of zero throughout mean dense rows)
-    is copied."""
+    is not dense, whose address or strides are not multiples of 16 bytes, whose
+    steps lie `far` bytes apart or more (None: however far), or that is one row for
+    all indexes (strides of zero throughout mean dense rows) is copied."""
     if t.dtype is not dtype or t.shape != shape or t.device != dev:
         _bad(t, shape, dev, dtype, name)
     if t.is_contiguous() and not t.data_ptr() & 15:
@@ -639,6 +642,8 @@ def _rows(t, shape, dev, dtype, name):
         ok = not ((sb | sh | sl) & unit or t.data_ptr() & 15) and (st[3] == 1 or shape[3] == 1)
     else:
         ok = True
+    if far is not None and sl * t.element_size() >= far:
+        ok = False
     if not (ok and (sb or sh or sl or shape[0] * shape[1] * shape[2] <= 1)) and t.numel():
         return _rows(t.clone(memory_format=torch.contiguous_format), shape, dev, dtype, name)
     return t, (sb, sh, sl)
@@ -886,8 +891,8 @@ class _Qk:
         B, Hq, L, d = q.shape
         Hk = k.shape[1]
         self.dev, self.d = dev, d
-        self.q, self.qs = _rows(q, q.shape, dev, dt, "q")
-        self.k, self.ks = _rows(k, (B, Hk, L, d), dev, dt, "k")
+        self.q, self.qs = _rows(q, q.shape, dev, dt, "q", None)
+        self.k, self.ks = _rows(k, (B, Hk, L, d), dev, dt, "k", None)
         self.wq, self.wk = _dev_param(wq, (d,), dev, "wq"), _dev_param(wk, (d,), dev, "wk")
         rot = pos = stride = bits = 0
         if inv_freq is not None:
@@ -950,8 +955,8 @@ def qk_norm_grads(q, k, dq, dk, *, wq=None, wk=None, norm="rms", eps=1e-6, posit
     _on_device("q, k, dq and dk", q, k, dq, dk)
     with _on(q.device, stream):
         c = _Qk(q, k, wq, wk, norm, eps, positions, inv_freq, interleaved)
-        dq, dqs = _rows(dq, c.q.shape, c.dev, c.q.dtype, "dq")
-        dk, dks = _rows(dk, c.k.shape, c.dev, c.q.dtype, "dk")
+        dq, dqs = _rows(dq, c.q.shape, c.dev, c.q.dtype, "dq", None)
+        dk, dks = _rows(dk, c.k.shape, c.dev, c.q.dtype, "dk", None)
         qo, qos, ko, kos = c.outputs(out)
         gw = [None if w is None else torch.empty(c.d, device=c.dev, dtype=torch.float32) for w in (wq, wk)]
         nbytes = lib().pgf_qk_norm_workspace_bytes(c.pack(qos, kos, dqs, dks))

@@ -12,7 +12,7 @@ namespace {
 constexpr int64_t kMaxItems = int64_t(1) << 30;
 constexpr int64_t kMaxHeads = int64_t(1) << 16, kMaxBatch = int64_t(1) << 24, kMaxLen = int64_t(1) << 32;
 constexpr int64_t kMaxStride = int64_t(1) << 44;
-constexpr int64_t kMaxStep = (int64_t(1) << 24) - 16;      // bytes from step to step
+constexpr int64_t kMaxStep = (int64_t(1) << 24) - 1;      // bytes from step to step
 constexpr size_t kMaxTotal = size_t(1) << 46;
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }

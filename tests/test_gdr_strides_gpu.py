@@ -119,3 +119,20 @@ def test_grads_into_rows_of_heads(dtype):
     got = binding.gdr_grads(*d, do, out=big.split(64, -1))
     assert all(torch.equal(x, y) for x, y in zip(got, want))
     assert torch.equal(big, torch.cat(want[:3], -1))
+
+
+def test_steps_far_apart():
+    """Inputs whose steps lie 2^24 bytes apart, as documented: any strides."""
+    c, d = make(1, 2, 2, 5, 64, 64, F32, seed=87)
+    big = torch.empty(5, 1 << 22, device=DEV)
+    far = []
+    for i, x in enumerate(d[:3]):
+        v = big[:, 128 * i:128 * (i + 1)].unflatten(1, (1, 2, 64)).permute(1, 2, 0, 3)
+        v.copy_(x)
+        far.append(v)
+    do = torch.randn(1, 2, 5, 64, device=DEV)
+    assert torch.equal(binding.gdr_scan(*far, *d[3:]), binding.gdr_scan(*d))
+    for x, y in zip(binding.gdr_grads(*far, *d[3:], do), binding.gdr_grads(*d, do)):
+        assert torch.equal(x, y)
+    S = [torch.zeros(1, 2, 64, 64, device=DEV) for _ in range(2)]
+    assert torch.equal(binding.gdr_step(*far, *d[3:], S[0]), binding.gdr_step(*d, S[1])) and torch.equal(*S)
