@@ -744,6 +744,8 @@ class _Gdr:
         self.B, self.cell = B, (B, Hv, dk, dv)
         self.scale = float(dk ** -0.5 if scale is None else scale)
         self.seg_len = int(seg_len)
+        if not -1 <= self.seg_len < 1 << 31:
+            raise ValueError("seg_len: -1, 0 or a multiple of 64 below 2^31")
         self.n_seqs = self.cu = 0
 
     def packed(self, c):

@@ -1,5 +1,7 @@
 """Arguments of the binding's gated delta rule that need no GPU: which inputs are
-read in place."""
+read in place, and
+numbers that the parameter block cannot hold."""
+import pytest
 import torch
 
 from paper_2512_23068_amd import binding
@@ -25,3 +27,10 @@ def test_far_steps_are_copied():
         gate.copy_(g)
         c = binding._Gdr(q, k, v, gate, beta, None, 0)
         assert (c.g.data_ptr() != gate.data_ptr()) == copied and torch.equal(c.g, g)
+
+
+def test_segments_beyond_the_parameter_block():
+    x = inputs()
+    for seg in (1 << 31, -1 << 40):
+        with pytest.raises(ValueError, match="seg_len"):
+            binding._Gdr(*x, None, seg)
