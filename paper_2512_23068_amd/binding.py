@@ -690,7 +690,7 @@ def _state(t, shape, dev, name):
 # host time is what a single token waits for.
 _GDR_PACK = struct.Struct("@7qPiifii27q5PqPPN")
 _QK_PACK = struct.Struct("@6qiiif18q4PiqPPPN")
-_HERE = contextlib.nullcontext()
+_AS_IT_IS = contextlib.nullcontext()
 # (without the check for a lazy start: there are device tensors already)
 _device_now = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
@@ -699,7 +699,7 @@ def _on(dev, stream):
     """Context of a call: the tensors' device and the caller's stream, where they
     are not current already."""
     if stream is None and dev.index == _device_now():
-        return _HERE
+        return _AS_IT_IS
     stack = contextlib.ExitStack()
     stack.enter_context(torch.cuda.device(dev))
     stack.enter_context(_on_stream(stream, dev))

@@ -220,12 +220,14 @@ __attribute__((amdgpu_waves_per_eu(sizeof(T) == 4 && DK == 128 ? 3 : 4))) void k
 // over the rows of the wave's own last result, which lies as the operand it is
 // needed as (see mfma), so nothing crosses waves but the staged chunk; the
 // next one is loaded into registers meanwhile.
-// Bound by issue: at 128 x 128 in bf16 a wave's chunk is 96 matrix instructions of
-// 16 cycles and about 300 vector ones of 2.4, of which half take S and X apart;
-// two waves on a SIMD need 3 us a chunk each, one alone 2 us.  4 x 4096 steps of 16
-// heads take 230 us (of 275 with the records), 131072 steps of 32 heads of 64 x 64
-// in f32 1.1 ms as kOut, there at the memory's rate (5.1 GB).  32 steps a chunk:
-// a longer one has fewer splits of S a step, and longer products with T^.
+// Bound by issue where two waves share a SIMD: at 128 x 128 in bf16 a wave's chunk is
+// 96 matrix instructions of 16 cycles and about 300 vector ones of 2.4, of which half
+// take S and X apart, and both need 3 us a chunk.  A wave that has its SIMD to itself
+// waits for its own last products instead: 2 us a chunk, or 1.9 with half of the work
+// (HS = 2), of which it issues for 1.1 (matrix cores 20 % busy).  4 x 4096 steps of 16
+// heads take 232 us (of 277 with the records), 131072 steps of 32 heads of 64 x 64 in
+// f32 1.1 ms as kOut, there at the memory's rate (5.1 GB).  32 steps a chunk: a longer
+// one has fewer splits of S a step, and longer products with T^.
 //   kOut      outputs, from the true entry state
 //   kSegment  zero-start end state of the segment (value columns) and its
 //             transition (columns of the identity, v = 0)
@@ -256,7 +258,7 @@ struct Chunk {
 // updating its keys and writing half the outputs.  A fifth more work for half the
 // chain: taken up to as many tiles as leave every SIMD at most one such wave (16
 // heads of 128 x 128, 2048 steps, us with one wave a tile and with two: 512 tiles
-// 153 and 139, 768 tiles 160 and 188, 1024 tiles 166 and 198).
+// 166 and 143, 768 tiles 173 and 195, 1024 tiles 178 and 202).
 template <typename T, int DK, int MODE, int HS>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_gdr_chain(Args a, uint32_t n_items) {
     using Ck = Chunk<T, DK, MODE>;
@@ -585,7 +587,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // S <- M S + E with the segments' transitions M and zero-start end states E
 // (E's place receives the entry state).  BACK: the adjoint leaving each, from
 // the last to the first, with M transposed.  A block has 16 value columns of a
-// head; its four waves share the keys and pass the state's parts through LDS.
+// head; its DK / 16 waves share the keys and pass the state's parts through LDS.
 // 1.4 us a segment at 128 x 128 (32 segments of 4 heads 43 us): its products wait
 // for the last segment's, and three segments are loaded ahead of them.  A block
 // reads 64 KB a segment, a thousand cycles of its CU's path to the cache where each

@@ -113,16 +113,16 @@ double pass(double waves, double chunks) {
 }
 
 // Steps per segment, 0 = not cut.  A wave takes 16 columns of one head through
-// its chunks one after the other, two that share a tile in 1.8 us each (the scan's
+// its chunks one after the other, two that share a tile in 1.9 us each (the scan's
 // outputs where they are as few as kShareTiles).  Cutting a sequence costs the
 // zero-start end states and the transitions (dk more columns, without outputs: 3/4
 // of the work a column) on top, the carry, 1.4 us a segment one after the other and
 // one block a CU, and two more launches.  Of the lengths below, that of the least
-// sum is taken.  Measured, dk = dv = 128, bf16, us: 4 heads of 1024 steps 70 uncut,
-// 57 in segments of 256; of 32768 steps 1715 uncut, 334 / 245 / 211 / 257 / 438 in
-// segments of 256 / 512 / 1024 / 2048 / 4096; 32 heads of 16384 steps 928 uncut,
-// 788 / 638 / 556 / 539 / 616; 4 x 16 heads of 4096 steps 261 uncut, 272 in segments
-// of 1024.
+// sum is taken.  Measured, dk = dv = 128, bf16, us: 4 heads of 1024 steps 74 uncut,
+// 57 in segments of 256; of 32768 steps 1785 uncut, 337 / 250 / 226 / 263 / 446 in
+// segments of 256 / 512 / 1024 / 2048 / 4096; 32 heads of 16384 steps 961 uncut,
+// 790 / 639 / 580 / 549 / 639; 4 x 16 heads of 4096 steps 272
+// uncut, 284 in segments of 1024.
 int64_t default_seg(const Plan &q, bool packed, bool grads) {
     const int64_t unit = kSuper * kC, steps = packed ? q.L : q.B * q.L;
     // Packed lengths are on the device: the longest is taken as four times the mean.

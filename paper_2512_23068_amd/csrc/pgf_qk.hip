@@ -60,7 +60,7 @@ constexpr int kPairs = 256;          // rotated pairs of a step at most
 // Cosine and sine of `turns` in [-1/2, 1/2], in f64 and rounded once: the nearest
 // quarter is taken off, exactly, and the series of the rest, at most pi / 4, leave
 // 2^-52 at the terms x^15 and x^16.  (The library's sincospi takes the adjoint more
-// registers than it has: 108 us in place of 102 for 4 x 4096 steps of 32 heads.)
+// registers than it has: 108 us in place of 103 for 4 x 4096 steps of 32 heads.)
 __device__ __forceinline__ float2 cos_sin(double turns) {
     const double n = rint(4.0 * turns);
     const double x = 6.28318530717958647693 * fma(-0.25, n, turns), z = x * x;
@@ -114,7 +114,8 @@ __device__ __forceinline__ void store4(T *p, const floatx4 &v) {
 }
 
 // Bound by memory: x is read and y written once (and dy read by the adjoint):
-// 16384 steps of 32 heads of 128 in bf16 72 us (3.7 TB/s), the adjoint 99 us (4.1).
+// 16384 steps of 32 heads of 128 in bf16 72 us (3.7 TB/s), the adjoint 99 us (4.1; a
+// few registers spill around the angles, 10 MB of 403, without which it takes as long).
 // The next vector is loaded while one is computed, the first ones while the
 // angles are.
 template <typename T, int G, bool GRAD>
