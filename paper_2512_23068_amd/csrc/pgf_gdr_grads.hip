@@ -13,10 +13,13 @@
 //   w_t  = e^{G_C - G_t} z_t + sum_{s>=t} scale c_st (dO_s.E_t) q_s - sum_{s>t} c_st (dE_s.E_t) k_s
 //   r_t  = -e^{G_t} y_t - sum_{u<t} c_tu beta_u (dE_t.E_u) k_u
 //   dk_t = beta_t w_t + r_t,   dbeta_t = k_t.w_t
-//   dG_t = q_t.dq_t + k_t.r_t - beta_t dbeta_t,  at the run's end also <dS1, S1>,
-//   dg   = sums of dG from each step to the run's end
-// (G_t enters wherever q_t reads the state or k_t reads it, against where k_t
-// writes it).  <dS1, S1> = e^{G_C} <dS1, S0> + sum_t e^{G_C - G_t} beta_t k_t.z_t.
+// dg_t is the sum of all that a step before t leaves to one from t on (each with the
+// decays between, g_t among them): what q_s and k_s read less what k_u, u >= t, wrote
+// of it, and what the steps before t and S0 leave to S1:
+//   dg_t = sum_{s>=t} (q_s.dq'_s + k_s.r_s - beta_s k_s.w'_s) + sum_{u<t} e^{G_C - G_u} beta_u k_u.z_u
+//          + e^{G_C} <dS1, S0>
+// Here dq' is dq without its term t = s, and w' is w without its terms s = t and z:
+// those have no decay and would cancel, and under strong decays dg is the small rest.
 //
 //   k_gdr_prep                records, with T^
 //   k_gdr_chain<kSave>        forward: E, and S every 64 steps
@@ -526,18 +529,22 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
     if (lane == 0) lds.dot[4 * SIDE + w] = ss;
     const double Gt = lds.G[tok], Gend = lds.G[kRun - 1];
     const float be = lds.be[tok];
-    // decays and signs of the 64 x 64 products; what has no place is zero
+    // decays and signs of the 64 x 64 products; what has no place is zero.  The step's
+    // own term, scale dO_t.E_t, stays apart.
+    float own = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int row = 16 * i + 4 * qd + j;
             const float dG = (float)(Gt - lds.G[row]);
-            const bool at = SIDE ? row >= tok : row <= tok;
+            const bool at = SIDE ? row > tok : row < tok;
             const float e = __builtin_amdgcn_exp2f(at ? (SIDE ? -dG : dG) : 0.0f) * (SIDE ? 1.0f : lds.be[row]);
+            own = row == tok ? d1[i][j] : own;
             d1[i][j] = at ? a.scale * e * d1[i][j] : 0.0f;
-            d2[i][j] = at && row != tok ? -e * d2[i][j] : 0.0f;
+            d2[i][j] = at ? -e * d2[i][j] : 0.0f;
         }
+    own = a.scale * (SIDE ? 1.0f : be) * __shfl(own, c / 4 * 16 + c, 64);
     lds_barrier();                             // phase one's reads
 #pragma unroll
     for (int i = 0; i < KU; ++i) {
@@ -630,6 +637,7 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
             for (int j = 0; j < 4; ++j) {
                 kr = fmaf(kx[j], x1[kt][j], kr);
                 qdq = fmaf(qx[j], x2[kt][j], qdq);
+                x2[kt][j] = fmaf(own, kx[j], x2[kt][j]);
             }
         }
         float s = qdq + kr;
@@ -649,7 +657,7 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
         keep(a.dq, accq, x2);
     } else {
         const float out = __builtin_amdgcn_exp2f((float)(Gend - Gt));
-        float kz = 0.0f, kw = 0.0f;
+        float kz = 0.0f, kw = 0.0f, kq = 0.0f;         // k.z, k.w', k.q
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
             const floatx4 kx = row4(lds.k.K, kt);
@@ -677,30 +685,39 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
                 const int x = kt / W & 1;
                 if (kt + W < KT) read(kt + W);
                 __builtin_amdgcn_sched_barrier(0);
-                floatx4 y[W];
+                floatx4 y[W], v[W];
 #pragma unroll
-                for (int i = 0; i < W; ++i) y[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
-                mfma_parts2<P, 3>(qf[x], f1, x1 + kt);
+                for (int i = 0; i < W; ++i) y[i] = v[i] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+                mfma_parts2<P, 3>(qf[x], f1, v);
                 mfma_parts2<P, 3>(kf[x], f2, y);
 #pragma unroll
-                for (int i = 0; i < W; ++i) x1[kt + i] += y[i];
+                for (int i = 0; i < W; ++i) {
+                    const floatx4 kx = row4(lds.k.K, kt + i), s = y[i] + v[i];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) kw = fmaf(kx[j], s[j], kw);
+                    x1[kt + i] += s;
+                }
             }
         }
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const floatx4 kx = row4(lds.k.K, kt);
+            const floatx4 kx = row4(lds.k.K, kt), qx = row4(lds.k.Q, kt);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) kw = fmaf(kx[j], x1[kt][j], kw);
+            for (int j = 0; j < 4; ++j) {
+                kq = fmaf(kx[j], qx[j], kq);
+                x1[kt][j] = fmaf(own, qx[j], x1[kt][j]);
+            }
         }
 #pragma unroll
         for (int m = 16; m < 64; m *= 2) {
             kz += __shfl_xor(kz, m, 64);
             kw += __shfl_xor(kw, m, 64);
+            kq += __shfl_xor(kq, m, 64);
         }
         if (qd == 0) {
             lds.dG[1][tok] = -be * kw;
             lds.kz[tok] = be * kz;
-            if (tok < live) a.dbeta[(r.b * a.Hv + h) * a.seqs.L + t0 + tok] = kw;
+            if (tok < live) a.dbeta[(r.b * a.Hv + h) * a.seqs.L + t0 + tok] = fmaf(own, kq, kz + kw);
         }
         floatx4 sum[KT];
 #pragma unroll
@@ -715,12 +732,12 @@ __device__ __forceinline__ void outer_side(const Args &a, OuterLds<T, DK> &lds, 
         }
         keep(a.dk_, acck, x1);
         if (w == vh % 4) {
-            double v = (double)lds.dG[0][lane] + lds.dG[1][lane], e = lds.kz[lane];
+            double v = (double)lds.dG[0][lane] + lds.dG[1][lane], e = lane ? lds.kz[lane - 1] : 0.0;
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) {
-                e += __shfl_xor(e, m, 64);
-                const double x = __shfl_down(v, m, 64);
+                const double x = __shfl_down(v, m, 64), y = __shfl_up(e, m, 64);
                 if (lane + m < 64) v += x;
+                if (lane >= m) e += y;
             }
             double s01 = 0.0;
 #pragma unroll

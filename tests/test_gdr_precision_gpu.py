@@ -1,5 +1,5 @@
-"""Roundings on the GPU: bf16 outputs of the gated delta rule, and the rotation of
-queries and keys.
+"""Roundings on the GPU: bf16 outputs of the gated delta rule, its gradients under
+strong decays, and the rotation of queries and keys.
 
 A bf16 input is the first of its f32 value's three parts and the other two are
 zero, so the scan of bf16 inputs and that of the same values in f32 add the same
@@ -9,7 +9,8 @@ import pytest
 import torch
 
 from paper_2512_23068_amd import binding
-from tests.test_gdr_gpu import BF16, DEV, make
+from tests.test_gdr_gpu import BF16, DEV, F32, TOL, check, make
+from tests.test_gdr_grads_gpu import compare, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -50,3 +51,25 @@ def test_rotation_is_rounded_once(il):
         worst = float((err / want.abs()).max())
         print(f"worst {worst * 2 ** 24:.3f} x 2^-24", flush=True)
         assert bool((err <= 2.0 ** -24 * want.abs() + 3 * 2.0 ** -53 * (ang + 2 * torch.pi)).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("strength", [0.5, 3.0, 10.0, 30.0])
+@pytest.mark.parametrize("Hk,Hv,L,dk,dv", [(2, 4, 130, 64, 64), (1, 1, 200, 128, 40), (1, 2, 33, 24, 200)])
+def test_gradient_of_strong_decays(dtype, strength, Hk, Hv, L, dk, dv):
+    """dl/dg falls with the decays: what one step leaves to the next, e^g of it.  Its
+    terms do as well, so its error stays that of sums of some hundred f32 terms of its
+    own size, 1e-5 as for every f32 output, head by head.  (The decays of a head are
+    within 10 % of each other, e^3 at the strongest.)"""
+    print(f"case {dtype} {strength} {Hk} {Hv} {L} {dk} {dv}", flush=True)
+    c, d = make(1, Hk, Hv, L, dk, dv, dtype, seed=72)
+    gen = torch.Generator().manual_seed(4)
+    g = -strength * (1 + 0.1 * torch.rand(1, Hv, L, generator=gen))
+    c, d = (*c[:3], g, c[4]), (*d[:3], g.to(DEV), d[4])
+    S0, dS1 = (torch.randn(1, Hv, dk, dv, generator=gen) for _ in range(2))
+    do = torch.randn(1, Hv, L, dv, generator=gen).to(dtype)
+    got = binding.gdr_grads(*d, do.to(DEV), S_in=S0.to(DEV), dS_out=dS1.to(DEV))
+    want = reference(c, do, dk ** -0.5, S0, dS1)
+    compare(got, want, dtype)
+    for h in range(Hv):
+        check(f"dg of head {h}", got[3][:, h], want[3][:, h], TOL[F32])
