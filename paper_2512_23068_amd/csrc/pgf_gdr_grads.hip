@@ -322,11 +322,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // three parts, which both sides read: the products with S0 (or dS1), and the
 // 64 x 64 products of E, dE and dO in the orientation the next product wants them
 // as operand.  Phase two adds the products with K and Q, and r passes to side 1.
-// At 128 x 128 in bf16 a block takes 94000 cycles, 29000 of them in a SIMD's
+// At 128 x 128 in bf16 a block takes about 95000 cycles, 29000 of them in a SIMD's
 // matrix instructions: the rest is the staging (7 instructions for two numbers'
 // parts) and the waits between the phases, which one block of eight waves a CU (all
 // that the registers hold) does not fill.  1024 blocks of two heads (2 x 4096
-// steps, 16 heads) take 187 us; two blocks of four waves a CU, one side after the
+// steps, 16 heads) take 190 us; two blocks of four waves a CU, one side after the
 // other with S0, E and dE read and split twice, took 220 us.
 constexpr int kRun = kC * kSuper;
 constexpr double kLog2e = 1.4426950408889634;
